@@ -61,14 +61,15 @@
 extern "C" {
 #endif
 
-typedef enum { GPPS_F32 = 0, GPPS_F64 = 1 } gpps_dtype;
+/* GPPS_BF16 (bfloat16) is an element type of the recognition operators only. */
+typedef enum { GPPS_F32 = 0, GPPS_F64 = 1, GPPS_BF16 = 2 } gpps_dtype;
 
 typedef enum {
     GPPS_OK = 0,
     GPPS_ERR_NULL = 1,      /* a required pointer is NULL                              */
     GPPS_ERR_SHAPE = 2,     /* N < 1, M < 1, Q < 1, Q > GPPS_MAX_Q or M > GPPS_MAX_M   */
     GPPS_ERR_HYPER = 3,     /* sigma_f2 or some l_q is not finite and > 0              */
-    GPPS_ERR_DTYPE = 4,     /* dt is not a gpps_dtype                                  */
+    GPPS_ERR_DTYPE = 4,     /* dt is not a gpps_dtype that the call takes              */
     GPPS_ERR_WORKSPACE = 5, /* workspace smaller than gpps_workspace_bytes()           */
     GPPS_ERR_ALIGN = 6,     /* workspace not 256-byte aligned or an array misaligned   */
     GPPS_ERR_HIP = 7,       /* a HIP runtime call or kernel launch failed              */
@@ -259,6 +260,108 @@ gpps_status gpps_bound(gpps_dtype dt, int64_t N, int64_t M, int64_t Q, int64_t D
                        void *L, void *dmu, void *dS, void *dZ, void *dsigma_f2, void *dl,
                        void *dbeta, int flags, void *workspace, size_t workspace_bytes,
                        void *stream);
+
+/*
+ * Recognition operators: what a network needs that computes q(x_n) from the data (so that mu_n
+ * and S_n are functions with shared weights and not parameters of their own), and its training.
+ *
+ * They differ from the calls above in this:
+ *   - dt selects the type of the rows' arrays: GPPS_F32, GPPS_F64 or GPPS_BF16.  Weights,
+ *     statistics and states (named below) are float beside float or bfloat16 rows, double beside
+ *     double ones, and so is all arithmetic; results are rounded once, to nearest even.
+ *   - Arrays of rows have a stride: row n of `x` begins at x + n * ldx elements, ldx >= D.  A
+ *     row's elements are neighbours.  Pointers need the element's alignment only.
+ *   - N may be 0.  Outputs must not overlap inputs (the norm's y may be x).
+ *   - 1 <= D <= GPPS_MAX_WIDTH, N D <= 2^40.
+ * Ownership, streams, errors and determinism are as above.
+ */
+#define GPPS_MAX_WIDTH 16384
+#define GPPS_REVERSE 8    /* gpps_recurrence: from each sequence's last row to its first */
+#define GPPS_MAXIMIZE 16  /* gpps_adamw: steps along the gradient                        */
+
+/*
+ * Layer norm of every row:
+ *   mean = sum x / D,  rstd = (sum (x - mean)^2 / D + eps)^-1/2,  y = (x - mean) rstd weight + bias
+ * weight, bias [D] may be NULL (ones, zeros), mean, rstd [N] too (not wanted).  eps: finite, >= 0.
+ */
+gpps_status gpps_layer_norm(gpps_dtype dt, int64_t N, int64_t D, const void *x, int64_t ldx,
+                            const void *weight, const void *bias, double eps, void *y, int64_t ldy,
+                            void *mean, void *rstd, void *stream);
+
+/*
+ * Its gradients, given dy = dL/dy and the forward call's mean and rstd: dx [N x D], and
+ * dweight = sum_n dy xh, dbias = sum_n dy [D], xh = (x - mean) rstd (either may be NULL: not
+ * wanted; with GPPS_ACCUMULATE they are added to).  weight may be NULL (ones).
+ */
+size_t gpps_layer_norm_workspace_bytes(gpps_dtype dt, int64_t N, int64_t D);
+gpps_status gpps_layer_norm_grads(gpps_dtype dt, int64_t N, int64_t D, const void *x, int64_t ldx,
+                                  const void *weight, const void *mean, const void *rstd,
+                                  const void *dy, int64_t lddy, void *dx, int64_t lddx,
+                                  void *dweight, void *dbias, int flags, void *workspace,
+                                  size_t workspace_bytes, void *stream);
+
+/*
+ * Gated linear recurrence over B packed sequences, every channel by itself:
+ *   h_t = a_t h_{t-1} + (1 - a_t) x_t,   a_t = 1 / (1 + exp(-gate_t))
+ * Sequence b is rows offsets[b] .. offsets[b+1]-1 of x, gate and h [N x D]; it may be empty.
+ * The state before its first row is h0[b] (h0 [B x D], or NULL: zero); h_last[b] (may be NULL:
+ * not wanted) is the state after its last row, h0[b] for an empty one.  A call with one row a
+ * sequence is a streaming step.  With GPPS_REVERSE rows are taken from the last to the first
+ * (h_last belongs to the first row then).
+ *
+ *   offsets [B + 1]   device, int64, or NULL (B = 1: one sequence of all rows).  They begin with 0,
+ *                     never fall and end with N.  The call cannot check that: other contents
+ *                     give unspecified results, but no access outside the arrays.
+ * States are independent between sequences: what is not finite in one stays in it.
+ */
+size_t gpps_recurrence_workspace_bytes(gpps_dtype dt, int64_t N, int64_t B, int64_t D);
+gpps_status gpps_recurrence(gpps_dtype dt, int64_t N, int64_t B, int64_t D, const void *x,
+                            int64_t ldx, const void *gate, int64_t ldg, const int64_t *offsets,
+                            const void *h0, void *h, int64_t ldh, void *h_last, int flags,
+                            void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Its gradients, given the forward call's arguments and h, dh = dL/dh (NULL: zero) and
+ * dh_last [B x D] = dL/dh_last (NULL: zero): dx, dgate [N x D] and dh0 [B x D] (may be NULL: not
+ * wanted; dh_last[b] for an empty sequence).
+ */
+gpps_status gpps_recurrence_grads(gpps_dtype dt, int64_t N, int64_t B, int64_t D, const void *x,
+                                  int64_t ldx, const void *gate, int64_t ldg, const void *h,
+                                  int64_t ldh, const void *dh, int64_t lddh,
+                                  const int64_t *offsets, const void *h0, const void *dh_last,
+                                  void *dx, int64_t lddx, void *dgate, int64_t lddg, void *dh0,
+                                  int flags, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * One AdamW step over `count` tensors, in place:
+ *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2
+ *   p = p (1 - lr weight_decay) - lr / (1 - beta1^step) m / (sqrt(v / (1 - beta2^step)) + eps)
+ * n, p, g, m, v, m_scale, v_scale: HOST arrays of `count` element counts (0: skipped) and device
+ * pointers.  dt: the type of every p (F32, F64, BF16); grad_dt that of every g (F32 or BF16
+ * beside F32 and BF16, F64 beside F64).  bits: how m and v are held.
+ *   32 (64 beside F64)  float (double) arrays of n elements; m_scale, v_scale are not read.
+ *   8                   in blocks of GPPS_ADAMW_BLOCK elements with one float scale each
+ *                       (m_scale[i], v_scale[i]: ceil(n / GPPS_ADAMW_BLOCK) of them, the block's
+ *                       largest |m| and largest v): m int8, standing for
+ *                       scale sgn(c) (|c| / 127)^2, v uint8 for scale (c / 255)^4.
+ *                       All zeros is the start.  Not beside F64.  The step uses m and v before
+ *                       they are rounded.  A block with a moment that is not finite stands for
+ *                       NaN in all of it from then on.
+ * step counts from 1.  lr, eps, weight_decay: finite and >= 0; 0 <= beta1, beta2 < 1.  With
+ * GPPS_MAXIMIZE g is negated.  No tensor may overlap another.  All arguments are checked before
+ * the first launch; 64 tensors share one.
+ */
+#define GPPS_ADAMW_BLOCK 256
+gpps_status gpps_adamw(gpps_dtype dt, gpps_dtype grad_dt, int bits, int64_t count, const int64_t *n,
+                       void *const *p, const void *const *g, void *const *m, void *const *v,
+                       float *const *m_scale, float *const *v_scale, int64_t step, double lr,
+                       double beta1, double beta2, double eps, double weight_decay, int flags,
+                       void *stream);
+
+/* The n values that 8-bit codes stand for: of a first moment (second = 0, int8) or a second one
+ * (second = 1, uint8). */
+gpps_status gpps_adamw_values(int second, int64_t n, const void *codes, const float *scale,
+                              float *out, void *stream);
 
 /* Kernel timing for benchmarks.  While enabled (on != 0), every kernel launch
  * of the library is bracketed by two HIP events recorded on the call's stream.

@@ -433,3 +433,8 @@ def psi_grads_views(mu, S, Zs, sigma_f2s, ls, dL_dpsi0s, dL_dPsi1s, dL_dPsi2s, *
         _ptrs(out["dZ"]), _ptrs(out["dsigma_f2"]), _ptrs(out["dl"]), _flags(path, accumulate),
         workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream)))
     return out
+
+
+from .operators import (AdamW, adamw_step, adamw_values, layer_norm, layer_norm_grads,  # noqa: E402,F401
+                        layer_norm_workspace_bytes, recurrence, recurrence_grads,
+                        recurrence_workspace_bytes)

@@ -1,0 +1,341 @@
+// AdamW over many tensors in one call, the two moments held in 32 bits (64 beside fp64
+// parameters) or in 8 bits.
+//
+//   m = b1 m + (1 - b1) g          v = b2 v + (1 - b2) g^2
+//   p = p (1 - lr wd) - lr / (1 - b1^t) * m / (sqrt(v) / sqrt(1 - b2^t) + eps)
+//
+// Every element is touched once, so the step is bound by its bytes: 28 of them for fp32
+// parameters and gradients with 32-bit moments, 16 with 8-bit ones.  A launch takes up to 64
+// tensors, whose pointers travel in the kernel's arguments (no table to upload, so a call
+// needs no workspace and no copy): a workgroup takes 2,048 neighbouring elements of one
+// tensor, which it finds from the tensors' first workgroups by bisection.
+//
+// 8-bit moments: the elements of a tensor in blocks of 256, each with two scales in fp32, the
+// block's largest |m| and largest v.  A code stands for
+//   m = s sgn(c) (|c| / 127)^2, |c| <= 127        v = s (c / 255)^4, 0 <= c <= 255
+// so the codes are dense near zero, where most moments of a block lie: the smallest |m| that
+// is not rounded to zero is 1.6e-5 of the block's largest, the smallest sqrt(v) is 1.5e-5 of
+// it.  A v above zero never gets the code of zero (its quotient m / sqrt(v) would be
+// unbounded in the next step).  The step itself uses the moments before their rounding.  A
+// wave takes a block of 256, four elements a lane, so the two maxima stay in its registers.
+// Codes come from single roundings in a fixed order (no fused multiply-add in this file's
+// moments), so a program can reproduce them exactly.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "elem.h"
+#include "internal.h"
+
+namespace {
+
+using gpps::bf16_t;
+using gpps::Elem;
+using gpps::Wide;
+
+constexpr int kTensors = 64;     // of one launch: 3.9 KB of arguments
+constexpr int kChunk = 2048;     // elements of one workgroup
+constexpr int kBlock = GPPS_ADAMW_BLOCK;
+
+struct Tensor {
+    void *p;
+    const void *g;
+    void *m, *v;
+    float *ms, *vs;
+    int64_t n;
+};
+
+struct Batch {
+    Tensor t[kTensors];
+    uint32_t first[kTensors];    // first workgroup of each tensor
+    int count;
+};
+
+template <typename A>
+struct Coef {
+    A b1, c1, b2, c2;            // beta1, 1 - beta1, beta2, 1 - beta2
+    A keep;                      // 1 - lr wd
+    A step;                      // lr / (1 - beta1^t)
+    A root;                      // 1 / sqrt(1 - beta2^t)
+    A eps;
+    A sign;                      // -1: maximise
+};
+
+__device__ inline float root_of(float x) { return sqrtf(x); }
+__device__ inline double root_of(double x) { return sqrt(x); }
+
+template <typename A>
+__device__ inline void moments(A g, A &m, A &v, const Coef<A> &c) {
+#pragma clang fp contract(off)
+    m = m * c.b1 + g * c.c1;
+    v = v * c.b2 + g * c.c2 * g;
+}
+
+template <typename A>
+__device__ inline A update(A p, A m, A v, const Coef<A> &c) {
+    return p * c.keep - m / (root_of(v) * c.root + c.eps) * c.step;
+}
+
+__device__ inline float value_m(int c, float s) {
+#pragma clang fp contract(off)
+    const float r = fabsf(float(c)) * (1.0f / 127.0f);
+    const float a = s * (r * r);
+    return c < 0 ? -a : c > 0 ? a : a * 0.0f;
+}
+__device__ inline float value_v(int c, float s) {
+#pragma clang fp contract(off)
+    const float r = float(c) * (1.0f / 255.0f);
+    const float r2 = r * r;
+    return s * (r2 * r2);
+}
+
+// The largest of a wave's values, NaN if any of them is.
+__device__ inline float wave_max(float x) {
+    for (int o = 1; o < 64; o <<= 1) {
+        const float y = __shfl_xor(x, o);
+        x = (y > x || y != y) ? y : x;
+    }
+    return x;
+}
+
+__device__ inline int tensor_of(const Batch &b, uint32_t block) {
+    int lo = 0, hi = b.count - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (b.first[mid] <= block) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
+}
+
+template <typename P, typename G>
+__global__ __launch_bounds__(256) void adamw_kernel(Batch b, Coef<typename Elem<P>::Acc> c) {
+    using A = typename Elem<P>::Acc;
+    using PS = typename Elem<P>::Store;
+    using GS = typename Elem<G>::Store;
+    const int k = tensor_of(b, blockIdx.x);
+    const Tensor t = b.t[k];
+    const int64_t i0 = int64_t(blockIdx.x - b.first[k]) * kChunk;
+    const int64_t i1 = i0 + kChunk < t.n ? i0 + kChunk : t.n;
+    for (int64_t i = i0 + threadIdx.x * 4; i < i1; i += 256 * 4) {
+        const int n = int(i1 - i < 4 ? i1 - i : 4);
+        auto p = gpps::load_some<PS, 4>((const PS *)t.p + i, n);
+        const auto g = gpps::load_some<GS, 4>((const GS *)t.g + i, n);
+        auto m = gpps::load_some<A, 4>((const A *)t.m + i, n);
+        auto v = gpps::load_some<A, 4>((const A *)t.v + i, n);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            A me = m[e], ve = v[e];
+            moments(A(Elem<G>::up(g[e])) * c.sign, me, ve, c);
+            p[e] = Elem<P>::down(update(A(Elem<P>::up(p[e])), me, ve, c));
+            m[e] = me;
+            v[e] = ve;
+        }
+        gpps::store_some<PS, 4>((PS *)t.p + i, n, p);
+        gpps::store_some<A, 4>((A *)t.m + i, n, m);
+        gpps::store_some<A, 4>((A *)t.v + i, n, v);
+    }
+}
+
+template <typename P, typename G>
+__global__ __launch_bounds__(256) void adamw8_kernel(Batch b, Coef<float> c) {
+    using PS = typename Elem<P>::Store;
+    using GS = typename Elem<G>::Store;
+    const int k = tensor_of(b, blockIdx.x);
+    const Tensor t = b.t[k];
+    const int64_t i0 = int64_t(blockIdx.x - b.first[k]) * kChunk;
+    const int64_t i1 = i0 + kChunk < t.n ? i0 + kChunk : t.n;
+    const int lane = threadIdx.x % 64;
+    for (int64_t i = i0 + threadIdx.x / 64 * kBlock; i < i1; i += 4 * kBlock) {
+        const int64_t at = i + lane * 4;
+        const int n = int(at >= i1 ? 0 : i1 - at < 4 ? i1 - at : 4);
+        auto p = gpps::load_some<PS, 4>((const PS *)t.p + at, n);
+        const auto g = gpps::load_some<GS, 4>((const GS *)t.g + at, n);
+        auto cm = gpps::load_some<int8_t, 4>((const int8_t *)t.m + at, n);
+        auto cv = gpps::load_some<uint8_t, 4>((const uint8_t *)t.v + at, n);
+        const float ms = t.ms[i / kBlock], vs = t.vs[i / kBlock];
+        float m[4], v[4], top_m = 0.0f, top_v = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            m[e] = v[e] = 0.0f;
+            if (e < n) {
+                m[e] = value_m(cm[e], ms);
+                v[e] = value_v(cv[e], vs);
+                moments(Elem<G>::up(g[e]) * c.sign, m[e], v[e], c);
+                p[e] = Elem<P>::down(update(Elem<P>::up(p[e]), m[e], v[e], c));
+            }
+            const float am = fabsf(m[e]);
+            top_m = (am > top_m || am != am) ? am : top_m;
+            top_v = (v[e] > top_v || v[e] != v[e]) ? v[e] : top_v;
+        }
+        top_m = wave_max(top_m);
+        top_v = wave_max(top_v);
+        // scales below the normal range have no reciprocal: such a block's moment is zero
+        if (top_m < __FLT_MIN__) top_m = 0.0f;
+        if (top_v < __FLT_MIN__) top_v = 0.0f;
+        const float im = top_m > 0.0f ? 1.0f / top_m : 0.0f, iv = top_v > 0.0f ? 1.0f / top_v : 0.0f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+#pragma clang fp contract(off)
+            // (a NaN or infinite scale keeps the block's values non-finite; its codes are clamped)
+            const float um = rintf(sqrtf(fabsf(m[e]) * im) * 127.0f);
+            const float uv = rintf(sqrtf(sqrtf(v[e] * iv)) * 255.0f);
+            const int qm = int(fminf(fmaxf(um, 0.0f), 127.0f));
+            int qv = int(fminf(fmaxf(uv, 0.0f), 255.0f));
+            if (v[e] > 0.0f && top_v > 0.0f && qv < 1) qv = 1;
+            cm[e] = int8_t(m[e] < 0.0f ? -qm : qm);
+            cv[e] = uint8_t(qv);
+        }
+        gpps::store_some<PS, 4>((PS *)t.p + at, n, p);
+        gpps::store_some<int8_t, 4>((int8_t *)t.m + at, n, cm);
+        gpps::store_some<uint8_t, 4>((uint8_t *)t.v + at, n, cv);
+        if (lane == 0) {
+            t.ms[i / kBlock] = top_m;
+            t.vs[i / kBlock] = top_v;
+        }
+    }
+}
+
+template <typename C>
+__global__ __launch_bounds__(256) void adamw_values_kernel(int64_t n, const C *__restrict__ codes,
+                                                           const float *__restrict__ scale,
+                                                           float *__restrict__ out) {
+    for (int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 4; i < n; i += int64_t(gridDim.x) * 1024) {
+        const int k = int(n - i < 4 ? n - i : 4);
+        const auto c = gpps::load_some<C, 4>(codes + i, k);
+        const float s = scale[i / kBlock];
+        Wide<float, 4>::type v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            v[e] = sizeof(C) == 1 && C(-1) < C(0) ? value_m(c[e], s) : value_v(c[e], s);
+        gpps::store_some<float, 4>(out + i, k, v);
+    }
+}
+
+template <typename A>
+Coef<A> coefficients(int64_t step, double lr, double b1, double b2, double eps, double wd, bool maximize) {
+    Coef<A> c;
+    c.b1 = A(b1);
+    c.c1 = A(1.0 - b1);
+    c.b2 = A(b2);
+    c.c2 = A(1.0 - b2);
+    c.keep = A(1.0 - lr * wd);
+    c.step = A(lr / (1.0 - std::pow(b1, double(step))));
+    c.root = A(1.0 / std::sqrt(1.0 - std::pow(b2, double(step))));
+    c.eps = A(eps);
+    c.sign = maximize ? A(-1) : A(1);
+    return c;
+}
+
+template <typename P, typename G>
+hipError_t launch(const Batch &b, uint32_t blocks, bool eight, int64_t step, double lr, double b1,
+                  double b2, double eps, double wd, bool maximize, hipStream_t st) {
+    gpps::TimedScope ts(st, eight ? "adamw8" : "adamw");
+    const auto c = coefficients<typename Elem<P>::Acc>(step, lr, b1, b2, eps, wd, maximize);
+    if constexpr (sizeof(typename Elem<P>::Acc) == 4) {
+        if (eight) {
+            adamw8_kernel<P, G><<<blocks, 256, 0, st>>>(b, c);
+            return hipGetLastError();
+        }
+    }
+    adamw_kernel<P, G><<<blocks, 256, 0, st>>>(b, c);
+    return hipGetLastError();
+}
+
+bool aligned(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+
+size_t elem_size(gpps_dtype dt) { return dt == GPPS_F64 ? 8 : dt == GPPS_BF16 ? 2 : 4; }
+
+bool open_unit(double x) { return x >= 0.0 && x < 1.0; }
+
+}  // namespace
+
+extern "C" {
+
+gpps_status gpps_adamw(gpps_dtype dt, gpps_dtype grad_dt, int bits, int64_t count, const int64_t *n,
+                       void *const *p, const void *const *g, void *const *m, void *const *v,
+                       float *const *m_scale, float *const *v_scale, int64_t step, double lr,
+                       double beta1, double beta2, double eps, double weight_decay, int flags,
+                       void *stream) {
+    const bool wide = dt == GPPS_F64;
+    if (dt != GPPS_F32 && dt != GPPS_F64 && dt != GPPS_BF16) return GPPS_ERR_DTYPE;
+    if (wide ? grad_dt != GPPS_F64 : grad_dt != GPPS_F32 && grad_dt != GPPS_BF16) return GPPS_ERR_DTYPE;
+    if (bits != (wide ? 64 : 32) && (wide || bits != 8)) return GPPS_ERR_DTYPE;
+    if (count < 0 || step < 1) return GPPS_ERR_SHAPE;
+    const bool eight = bits == 8;
+    if (count && (!n || !p || !g || !m || !v || (eight && (!m_scale || !v_scale)))) return GPPS_ERR_NULL;
+    if (!std::isfinite(lr) || lr < 0.0 || !open_unit(beta1) || !open_unit(beta2) || !std::isfinite(eps) ||
+        eps < 0.0 || !std::isfinite(weight_decay) || weight_decay < 0.0)
+        return GPPS_ERR_HYPER;
+    if (flags & ~GPPS_MAXIMIZE) return GPPS_ERR_PATH;
+    const size_t pe = elem_size(dt), ge = elem_size(grad_dt), me = eight ? 1 : wide ? 8 : 4;
+    for (int64_t i = 0; i < count; ++i) {
+        if (n[i] < 0) return GPPS_ERR_SHAPE;
+        if (n[i] == 0) continue;
+        if (!p[i] || !g[i] || !m[i] || !v[i] || (eight && (!m_scale[i] || !v_scale[i]))) return GPPS_ERR_NULL;
+        if (!aligned(p[i], pe) || !aligned(g[i], ge) || !aligned(m[i], me) || !aligned(v[i], me) ||
+            (eight && (!aligned(m_scale[i], 4) || !aligned(v_scale[i], 4))))
+            return GPPS_ERR_ALIGN;
+    }
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    Batch b;
+    b.count = 0;
+    int64_t blocks = 0, i = 0, done = 0;                     // done: elements of tensor i already taken
+    while (i < count || b.count) {
+        if (i < count) {
+            if (n[i] == done) {
+                ++i;
+                done = 0;
+                continue;
+            }
+            const int64_t room = (gpps::kMaxBlocks - blocks) * kChunk;
+            const int64_t take = std::min(n[i] - done, room);
+            if (b.count < kTensors && take > 0) {
+                b.t[b.count] = Tensor{(char *)p[i] + done * pe, (const char *)g[i] + done * ge,
+                                      (char *)m[i] + done * me, (char *)v[i] + done * me,
+                                      eight ? m_scale[i] + done / kBlock : nullptr,
+                                      eight ? v_scale[i] + done / kBlock : nullptr, take};
+                b.first[b.count++] = uint32_t(blocks);
+                blocks += (take + kChunk - 1) / kChunk;
+                done += take;
+                continue;
+            }
+        }
+        const bool mx = flags & GPPS_MAXIMIZE;
+        hipError_t e;
+        const uint32_t nb = uint32_t(blocks);
+        if (wide)
+            e = launch<double, double>(b, nb, false, step, lr, beta1, beta2, eps, weight_decay, mx, st);
+        else if (dt == GPPS_F32 && grad_dt == GPPS_F32)
+            e = launch<float, float>(b, nb, eight, step, lr, beta1, beta2, eps, weight_decay, mx, st);
+        else if (dt == GPPS_F32)
+            e = launch<float, bf16_t>(b, nb, eight, step, lr, beta1, beta2, eps, weight_decay, mx, st);
+        else if (grad_dt == GPPS_F32)
+            e = launch<bf16_t, float>(b, nb, eight, step, lr, beta1, beta2, eps, weight_decay, mx, st);
+        else
+            e = launch<bf16_t, bf16_t>(b, nb, eight, step, lr, beta1, beta2, eps, weight_decay, mx, st);
+        if (e != hipSuccess) return GPPS_ERR_HIP;
+        b.count = 0;
+        blocks = 0;
+    }
+    return GPPS_OK;
+}
+
+gpps_status gpps_adamw_values(int second, int64_t n, const void *codes, const float *scale, float *out,
+                              void *stream) {
+    if (n < 0 || (second != 0 && second != 1)) return GPPS_ERR_SHAPE;
+    if (n == 0) return GPPS_OK;
+    if (!codes || !scale || !out) return GPPS_ERR_NULL;
+    if (!aligned(scale, 4) || !aligned(out, 4)) return GPPS_ERR_ALIGN;
+    const unsigned blocks = unsigned(std::min<int64_t>((n + 1023) / 1024, 1 << 16));
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    gpps::TimedScope ts(st, "adamw_values");
+    if (second)
+        adamw_values_kernel<<<blocks, 256, 0, st>>>(n, (const uint8_t *)codes, scale, out);
+    else
+        adamw_values_kernel<<<blocks, 256, 0, st>>>(n, (const int8_t *)codes, scale, out);
+    return hipGetLastError() == hipSuccess ? GPPS_OK : GPPS_ERR_HIP;
+}
+
+}  // extern "C"

@@ -363,10 +363,10 @@ const char *gpps_status_string(gpps_status status) {
     switch (status) {
         case GPPS_OK: return "success";
         case GPPS_ERR_NULL: return "a required pointer is NULL";
-        case GPPS_ERR_SHAPE: return "invalid shape (need 1 <= N, 1 <= M <= GPPS_MAX_M, 1 <= Q <= GPPS_MAX_Q, 1 <= D <= GPPS_MAX_D)";
-        case GPPS_ERR_HYPER: return "sigma_f2, every l_q, dL_dpsi0, beta and jitter must be finite; sigma_f2, l_q, beta > 0, jitter >= 0";
-        case GPPS_ERR_DTYPE: return "unknown dtype";
-        case GPPS_ERR_WORKSPACE: return "workspace smaller than gpps_workspace_bytes()";
+        case GPPS_ERR_SHAPE: return "invalid shape (need 1 <= N, 1 <= M <= GPPS_MAX_M, 1 <= Q <= GPPS_MAX_Q, 1 <= D <= GPPS_MAX_D; recognition operators: 0 <= N, 1 <= D <= GPPS_MAX_WIDTH, strides >= D, 1 <= B, 1 <= step)";
+        case GPPS_ERR_HYPER: return "sigma_f2, every l_q, dL_dpsi0, beta and jitter must be finite; sigma_f2, l_q, beta > 0, jitter >= 0 (lr, eps, weight_decay finite and >= 0; 0 <= beta1, beta2 < 1)";
+        case GPPS_ERR_DTYPE: return "unknown dtype, or one that this call does not take";
+        case GPPS_ERR_WORKSPACE: return "workspace smaller than the call's workspace query returns";
         case GPPS_ERR_ALIGN: return "workspace not 256-byte aligned or array not element-aligned";
         case GPPS_ERR_HIP: return "HIP runtime error or kernel launch failure";
         case GPPS_ERR_PATH: return "unknown flag bits, both path flags, or the requested path cannot run this call";

@@ -1,0 +1,441 @@
+"""Recognition operators: what a network needs that computes q(x_n) from the data.
+
+    layer_norm(x, weight, bias, eps)              -> (y, mean, rstd)
+    layer_norm_grads(x, weight, mean, rstd, dy)   -> dict(dx, dweight, dbias)
+    recurrence(x, gate, offsets, h0)              -> (h, h_last)
+    recurrence_grads(x, gate, h, dh, offsets, h0, dh_last) -> dict(dx, dgate, dh0)
+    adamw_step(params, grads, m, v, step, lr)     (in place)
+    AdamW(params, lr, bits=32 or 8)               the same with its moments kept
+    adamw_values(codes, scale)                    what 8-bit moments stand for
+
+Thin bindings over ``include/gpps.h`` like the rest of the package: they check
+tensors, allocate outputs and workspace, and pass pointers and the stream.  Rows
+may be float32, float64 or bfloat16 and strided (a column slice of a wider
+array); weights, statistics and states are float32 beside float32 and bfloat16
+rows and float64 beside float64 ones.  Tensors have to be on the current device.
+A call with ``stream=`` allocates on that stream and marks its arguments as used
+there.
+"""
+from __future__ import annotations
+
+import ctypes
+
+from . import F32, F64, GppsError, _check, _dev_tensor, lib, status_string
+
+BF16 = 2
+ACCUMULATE, REVERSE, MAXIMIZE = 1, 8, 16
+MAX_WIDTH = 16384
+ADAMW_BLOCK = 256
+
+_declared = None
+
+
+def _lib():
+    """The library with the argument types of these entry points set."""
+    global _declared
+    if _declared is not None:
+        return _declared
+    L = lib()
+    i64, vp, d, sz, i32 = ctypes.c_int64, ctypes.c_void_p, ctypes.c_double, ctypes.c_size_t, ctypes.c_int
+    L.gpps_layer_norm.argtypes = [i32, i64, i64, vp, i64, vp, vp, d, vp, i64, vp, vp, vp]
+    L.gpps_layer_norm_workspace_bytes.argtypes = [i32, i64, i64]
+    L.gpps_layer_norm_workspace_bytes.restype = sz
+    L.gpps_layer_norm_grads.argtypes = [i32, i64, i64, vp, i64, vp, vp, vp, vp, i64, vp, i64, vp, vp, i32,
+                                        vp, sz, vp]
+    L.gpps_recurrence_workspace_bytes.argtypes = [i32, i64, i64, i64]
+    L.gpps_recurrence_workspace_bytes.restype = sz
+    L.gpps_recurrence.argtypes = [i32, i64, i64, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp, i32, vp, sz, vp]
+    L.gpps_recurrence_grads.argtypes = [i32, i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp,
+                                        vp, i64, vp, i64, vp, i32, vp, sz, vp]
+    L.gpps_adamw.argtypes = [i32, i32, i32, i64, vp, vp, vp, vp, vp, vp, vp, i64, d, d, d, d, d, i32, vp]
+    L.gpps_adamw_values.argtypes = [i32, i64, vp, vp, vp, vp]
+    for name in ("layer_norm", "layer_norm_grads", "recurrence", "recurrence_grads", "adamw", "adamw_values"):
+        getattr(L, "gpps_" + name).restype = i32
+    _declared = L
+    return L
+
+
+def _row_dt(dtype) -> int:
+    import torch
+    if dtype == torch.float32:
+        return F32
+    if dtype == torch.float64:
+        return F64
+    if dtype == torch.bfloat16:
+        return BF16
+    raise TypeError(f"unsupported dtype {dtype}")
+
+
+def _wide(dtype):
+    import torch
+    return torch.float64 if dtype == torch.float64 else torch.float32
+
+
+def _first(x, name):
+    """Type, device and shape of the array that the others are checked against."""
+    import torch
+    if not isinstance(x, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if x.device.type != "cuda":
+        raise ValueError(f"{name} must be a GPU tensor (got {x.device})")
+    if x.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {x.device}, which is not the current device")
+    if x.dim() != 2:
+        raise ValueError(f"{name}: expected rows [N, D], got shape {tuple(x.shape)}")
+    return x.dtype, x.device, x.shape[0], x.shape[1]
+
+
+def _ld(x, name, dtype, shape, device) -> int:
+    """Checks an array of rows and returns the stride of its rows."""
+    import torch
+    if not isinstance(x, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if x.device != device or x.dtype != dtype:
+        raise ValueError(f"{name}: expected {dtype} on {device}, got {x.dtype} on {x.device}")
+    if tuple(x.shape) != shape:
+        raise ValueError(f"{name}: expected shape {shape}, got {tuple(x.shape)}")
+    N, D = shape
+    if (D > 1 and x.stride(1) != 1) or (N > 1 and x.stride(0) < D):
+        raise ValueError(f"{name}: a row's elements must be neighbours and rows must not overlap "
+                         f"(strides {x.stride()})")
+    return x.stride(0) if N > 1 else D
+
+
+def _ptr(x):
+    return None if x is None else x.data_ptr()
+
+
+def _current(device):
+    import torch
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+def _on_stream(stream, tensors, call):
+    """call() with `stream` as the current one; the tensors' memory is kept until it is done with them."""
+    import torch
+    for t in tensors:
+        if isinstance(t, torch.Tensor) and t.device.type == "cuda":
+            t.record_stream(stream)
+    with torch.cuda.stream(stream):
+        return call()
+
+
+def _scratch(need, workspace, device):
+    import torch
+    if need == 0:
+        raise GppsError(2, status_string(2))
+    if workspace is None:
+        return torch.empty(need, dtype=torch.uint8, device=device), need
+    if workspace.device != device or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous and on {device}")
+    have = workspace.numel() * workspace.element_size()
+    if have < need:
+        raise ValueError(f"workspace too small: need {need} bytes")
+    return workspace, have
+
+
+# ------------------------------------------------------------------ layer norm
+
+def layer_norm(x, weight=None, bias=None, eps=1e-5, *, out=None, stream=None):
+    """Layer norm of the rows of x [N x D].
+
+    Returns (y [N x D], mean [N], rstd [N]); ``out`` is such a triple to write into
+    (y may be x)."""
+    import torch
+    if stream is not None:
+        return _on_stream(stream, (x, weight, bias, *(out or ())),
+                          lambda: layer_norm(x, weight, bias, eps, out=out))
+    dtype, device, N, D = _first(x, "x")
+    dt, wide = _row_dt(dtype), _wide(dtype)
+    ldx = _ld(x, "x", dtype, (N, D), device)
+    if weight is not None:
+        _dev_tensor(weight, "weight", wide, (D,), device)
+    if bias is not None:
+        _dev_tensor(bias, "bias", wide, (D,), device)
+    if out is None:
+        y = torch.empty((N, D), dtype=dtype, device=device)
+        stats = torch.empty((2, N), dtype=wide, device=device)
+        mean, rstd = stats[0], stats[1]
+        ldy = D
+    else:
+        y, mean, rstd = out
+        ldy = _ld(y, "y", dtype, (N, D), device)
+        _dev_tensor(mean, "mean", wide, (N,), device)
+        _dev_tensor(rstd, "rstd", wide, (N,), device)
+    _check(_lib().gpps_layer_norm(dt, N, D, x.data_ptr(), ldx, _ptr(weight), _ptr(bias), float(eps), y.data_ptr(),
+                                  ldy, mean.data_ptr(), rstd.data_ptr(), _current(device)))
+    return y, mean, rstd
+
+
+def layer_norm_workspace_bytes(dtype, N: int, D: int) -> int:
+    return int(_lib().gpps_layer_norm_workspace_bytes(_row_dt(dtype), N, D))
+
+
+def layer_norm_grads(x, weight, mean, rstd, dy, *, bias=True, accumulate=False, out=None, workspace=None,
+                     stream=None):
+    """Gradients of ``layer_norm`` from its x, weight, mean and rstd and dy = dL/dy.
+
+    Returns a dict with dx [N x D], dweight [D] (None when weight is None) and dbias
+    [D] (None with ``bias=False``).  With ``accumulate=True`` and ``out`` (such a
+    dict) dweight and dbias are added to."""
+    import torch
+    if stream is not None:
+        return _on_stream(stream, (x, weight, mean, rstd, dy, workspace, *(out or {}).values()),
+                          lambda: layer_norm_grads(x, weight, mean, rstd, dy, bias=bias, accumulate=accumulate,
+                                                   out=out, workspace=workspace))
+    dtype, device, N, D = _first(x, "x")
+    dt, wide = _row_dt(dtype), _wide(dtype)
+    ldx = _ld(x, "x", dtype, (N, D), device)
+    lddy = _ld(dy, "dy", dtype, (N, D), device)
+    if weight is not None:
+        _dev_tensor(weight, "weight", wide, (D,), device)
+    _dev_tensor(mean, "mean", wide, (N,), device)
+    _dev_tensor(rstd, "rstd", wide, (N,), device)
+    if out is None:
+        new = torch.zeros if accumulate else torch.empty
+        out = {"dx": torch.empty((N, D), dtype=dtype, device=device),
+               "dweight": new(D, dtype=wide, device=device) if weight is not None else None,
+               "dbias": new(D, dtype=wide, device=device) if bias else None}
+    else:
+        for k in ("dweight", "dbias"):
+            if out[k] is not None:
+                _dev_tensor(out[k], k, wide, (D,), device)
+    lddx = _ld(out["dx"], "dx", dtype, (N, D), device)
+    ws, ws_bytes = _scratch(layer_norm_workspace_bytes(dtype, N, D), workspace, device)
+    _check(_lib().gpps_layer_norm_grads(
+        dt, N, D, x.data_ptr(), ldx, _ptr(weight), mean.data_ptr(), rstd.data_ptr(), dy.data_ptr(), lddy,
+        out["dx"].data_ptr(), lddx, _ptr(out["dweight"]), _ptr(out["dbias"]), ACCUMULATE if accumulate else 0,
+        ws.data_ptr(), ws_bytes, _current(device)))
+    return out
+
+
+# ------------------------------------------------------------------ recurrence
+
+def recurrence_workspace_bytes(dtype, N: int, B: int, D: int) -> int:
+    return int(_lib().gpps_recurrence_workspace_bytes(_row_dt(dtype), N, B, D))
+
+
+def _sequences(offsets, device) -> int:
+    """Checks the offsets (their contents are the caller's, on the device) and returns how many sequences they mark."""
+    import torch
+    if offsets is None:
+        return 1
+    if not isinstance(offsets, torch.Tensor):
+        raise TypeError("offsets must be a torch.Tensor")
+    if offsets.device != device or offsets.dtype != torch.int64:
+        raise ValueError(f"offsets: expected torch.int64 on {device}, got {offsets.dtype} on {offsets.device}")
+    if offsets.dim() != 1 or offsets.shape[0] < 2 or not offsets.is_contiguous():
+        raise ValueError("offsets: expected contiguous [B + 1] with B >= 1")
+    return offsets.shape[0] - 1
+
+
+def recurrence(x, gate, offsets=None, h0=None, *, reverse=False, out=None, workspace=None, stream=None):
+    """h_t = a_t h_{t-1} + (1 - a_t) x_t, a_t = sigmoid(gate_t), over packed sequences.
+
+    x, gate [N x D]; sequence b is rows offsets[b] .. offsets[b+1]-1 (``offsets``
+    int64 [B + 1] on the device, from 0 to N without falling, sequences may be empty;
+    None: one sequence of all rows).  ``h0`` [B x D]: the states before the first
+    rows (None: zero).  Returns (h [N x D], h_last [B x D]), h_last the states after
+    the last rows, so a stream of rows is taken in pieces (down to one row a call) by
+    handing h_last on as h0.  ``reverse=True`` takes rows from last to first."""
+    import torch
+    if stream is not None:
+        return _on_stream(stream, (x, gate, offsets, h0, workspace, *(out or ())),
+                          lambda: recurrence(x, gate, offsets, h0, reverse=reverse, out=out, workspace=workspace))
+    dtype, device, N, D = _first(x, "x")
+    dt, wide = _row_dt(dtype), _wide(dtype)
+    ldx = _ld(x, "x", dtype, (N, D), device)
+    ldg = _ld(gate, "gate", dtype, (N, D), device)
+    B = _sequences(offsets, device)
+    if h0 is not None:
+        _dev_tensor(h0, "h0", wide, (B, D), device)
+    if out is None:
+        h = torch.empty((N, D), dtype=dtype, device=device)
+        h_last = torch.empty((B, D), dtype=wide, device=device)
+        ldh = D
+    else:
+        h, h_last = out
+        ldh = _ld(h, "h", dtype, (N, D), device)
+        _dev_tensor(h_last, "h_last", wide, (B, D), device)
+    ws, ws_bytes = _scratch(recurrence_workspace_bytes(dtype, N, B, D), workspace, device)
+    _check(_lib().gpps_recurrence(dt, N, B, D, x.data_ptr(), ldx, gate.data_ptr(), ldg, _ptr(offsets), _ptr(h0),
+                                  h.data_ptr(), ldh, h_last.data_ptr(), REVERSE if reverse else 0, ws.data_ptr(),
+                                  ws_bytes, _current(device)))
+    return h, h_last
+
+
+def recurrence_grads(x, gate, h, dh, offsets=None, h0=None, dh_last=None, *, reverse=False, out=None,
+                     workspace=None, stream=None):
+    """Gradients of ``recurrence`` from its arguments, its h, dh = dL/dh [N x D] (None:
+    zero) and dh_last = dL/dh_last [B x D] (None: zero).
+
+    Returns a dict with dx, dgate [N x D] and dh0 [B x D]; ``out`` is such a dict to
+    write into (its dh0 may be None)."""
+    import torch
+    if stream is not None:
+        return _on_stream(stream, (x, gate, h, dh, offsets, h0, dh_last, workspace, *(out or {}).values()),
+                          lambda: recurrence_grads(x, gate, h, dh, offsets, h0, dh_last, reverse=reverse, out=out,
+                                                   workspace=workspace))
+    dtype, device, N, D = _first(x, "x")
+    dt, wide = _row_dt(dtype), _wide(dtype)
+    ldx = _ld(x, "x", dtype, (N, D), device)
+    ldg = _ld(gate, "gate", dtype, (N, D), device)
+    ldh = _ld(h, "h", dtype, (N, D), device)
+    lddh = D if dh is None else _ld(dh, "dh", dtype, (N, D), device)
+    B = _sequences(offsets, device)
+    for t, name in ((h0, "h0"), (dh_last, "dh_last")):
+        if t is not None:
+            _dev_tensor(t, name, wide, (B, D), device)
+    if out is None:
+        out = {"dx": torch.empty((N, D), dtype=dtype, device=device),
+               "dgate": torch.empty((N, D), dtype=dtype, device=device),
+               "dh0": torch.empty((B, D), dtype=wide, device=device)}
+        lddx = lddg = D
+    else:
+        lddx = _ld(out["dx"], "dx", dtype, (N, D), device)
+        lddg = _ld(out["dgate"], "dgate", dtype, (N, D), device)
+        if out["dh0"] is not None:
+            _dev_tensor(out["dh0"], "dh0", wide, (B, D), device)
+    ws, ws_bytes = _scratch(recurrence_workspace_bytes(dtype, N, B, D), workspace, device)
+    _check(_lib().gpps_recurrence_grads(
+        dt, N, B, D, x.data_ptr(), ldx, gate.data_ptr(), ldg, h.data_ptr(), ldh, _ptr(dh), lddh, _ptr(offsets),
+        _ptr(h0), _ptr(dh_last), out["dx"].data_ptr(), lddx, out["dgate"].data_ptr(), lddg, _ptr(out["dh0"]),
+        REVERSE if reverse else 0, ws.data_ptr(), ws_bytes, _current(device)))
+    return out
+
+
+# ------------------------------------------------------------------ AdamW
+
+def _held(t, what, i, dtype, n, device):
+    if t.dtype != dtype or t.device != device or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{what}[{i}]: expected contiguous {dtype} on {device} with {n} elements, got "
+                         f"{t.dtype} on {t.device} with {t.numel()}")
+    return t.data_ptr()
+
+
+def adamw_step(params, grads, m, v, step, lr, *, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01,
+               maximize=False, m_scale=None, v_scale=None, stream=None):
+    """One AdamW step over lists of tensors, in place.
+
+      m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2
+      p = p (1 - lr weight_decay) - lr / (1 - beta1^step) m / (sqrt(v / (1 - beta2^step)) + eps)
+
+    ``step`` counts from 1.  params: float32, float64 or bfloat16; a gradient is of the
+    same type, or float32 / bfloat16 beside bfloat16 / float32, or None (that tensor is
+    left as it is).  m, v: float32 (float64 beside float64 parameters), or, with
+    ``m_scale`` and ``v_scale``, 8-bit codes: m int8, v uint8, and a float32 scale for
+    each block of 256 elements (``AdamW(bits=8)`` makes them; ``adamw_values`` reads
+    them).  Every tensor is contiguous and none overlaps another."""
+    import torch
+    if stream is not None:
+        every = [t for l in (params, grads, m, v, m_scale or (), v_scale or ()) for t in l]
+        return _on_stream(stream, every, lambda: adamw_step(
+            params, grads, m, v, step, lr, betas=betas, eps=eps, weight_decay=weight_decay, maximize=maximize,
+            m_scale=m_scale, v_scale=v_scale))
+    eight = m_scale is not None
+    if eight != (v_scale is not None):
+        raise ValueError("m_scale and v_scale go together")
+    count = len(params)
+    lists = (grads, m, v) + ((m_scale, v_scale) if eight else ())
+    if any(len(l) != count for l in lists):
+        raise ValueError("params, grads, m, v (and the scales) must be lists of one length")
+    groups = {}
+    device = None
+    for i in range(count):
+        p, g = params[i], grads[i]
+        if g is None:
+            continue
+        if device is None:
+            device = p.device
+            if device.type != "cuda":
+                raise ValueError(f"params[{i}] must be a GPU tensor (got {device})")
+            if device.index != torch.cuda.current_device():
+                raise ValueError(f"params[{i}] is on {device}, which is not the current device")
+        dtype, gtype, n = p.dtype, g.dtype, p.numel()
+        group = groups.get((dtype, gtype))
+        if group is None:
+            _row_dt(dtype)
+            if gtype != dtype and {dtype, gtype} != {torch.float32, torch.bfloat16}:
+                raise TypeError(f"grads[{i}]: {gtype} beside parameters of {dtype}")
+            if eight and dtype == torch.float64:
+                raise TypeError(f"params[{i}]: 8-bit moments are held beside float32 and bfloat16 parameters only")
+            group = groups[dtype, gtype] = ([], [], [], [], [], [], [])
+        wide = _wide(dtype)
+        group[0].append(n)
+        group[1].append(_held(p, "params", i, dtype, n, device))
+        group[2].append(_held(g, "grads", i, gtype, n, device))
+        group[3].append(_held(m[i], "m", i, torch.int8 if eight else wide, n, device))
+        group[4].append(_held(v[i], "v", i, torch.uint8 if eight else wide, n, device))
+        if eight:
+            blocks = -(-n // ADAMW_BLOCK)
+            group[5].append(_held(m_scale[i], "m_scale", i, torch.float32, blocks, device))
+            group[6].append(_held(v_scale[i], "v_scale", i, torch.float32, blocks, device))
+    if not groups:
+        return
+    for group in groups.values():
+        some = [q for q, n in zip(group[1], group[0]) if n]
+        if len(set(some)) < len(some):
+            raise ValueError("a tensor is listed twice")
+    st = _current(device)
+    L = _lib()
+    for (dtype, gtype), group in groups.items():
+        k = len(group[0])
+        arrays = [(ctypes.c_int64 * k)(*group[0])] + [(ctypes.c_void_p * k)(*a) if a else None for a in group[1:]]
+        bits = 8 if eight else 64 if dtype == torch.float64 else 32
+        _check(L.gpps_adamw(_row_dt(dtype), _row_dt(gtype), bits, k, *arrays, int(step), float(lr), float(betas[0]),
+                            float(betas[1]), float(eps), float(weight_decay), MAXIMIZE if maximize else 0, st))
+
+
+def adamw_values(codes, scale, *, out=None, stream=None):
+    """The float32 values that 8-bit moments stand for: of a first moment (int8 codes) or
+    a second one (uint8), with their scales."""
+    import torch
+    if stream is not None:
+        return _on_stream(stream, (codes, scale, out), lambda: adamw_values(codes, scale, out=out))
+    if codes.dtype not in (torch.int8, torch.uint8):
+        raise TypeError(f"codes: expected torch.int8 or torch.uint8, got {codes.dtype}")
+    device, n = codes.device, codes.numel()
+    if device.type != "cuda" or device.index != torch.cuda.current_device():
+        raise ValueError(f"codes must be on the current GPU (got {device})")
+    _held(codes, "codes", 0, codes.dtype, n, device)
+    _held(scale, "scale", 0, torch.float32, -(-n // ADAMW_BLOCK), device)
+    if out is None:
+        out = torch.empty(codes.shape, dtype=torch.float32, device=device)
+    else:
+        _dev_tensor(out, "out", torch.float32, tuple(codes.shape), device)
+    _check(_lib().gpps_adamw_values(1 if codes.dtype == torch.uint8 else 0, n, codes.data_ptr(), scale.data_ptr(),
+                                    out.data_ptr(), _current(device)))
+    return out
+
+
+class AdamW:
+    """AdamW over a list of tensors, with the moments kept between steps.
+
+    ``bits=32``: moments in float32 (float64 beside float64 parameters); ``bits=8``: in
+    8 bits with a scale for each 256 elements (float32 and bfloat16 parameters).
+    ``step(grads)`` updates the parameters in place; ``m``, ``v``, ``m_scale``,
+    ``v_scale`` (None unless 8 bits) and ``steps`` are its whole state."""
+
+    def __init__(self, params, lr=1e-3, *, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, bits=32,
+                 maximize=False):
+        import torch
+        if bits not in (8, 32):
+            raise ValueError(f"bits: 8 or 32, got {bits}")
+        self.params = list(params)
+        self.lr, self.betas, self.eps = lr, betas, eps
+        self.weight_decay, self.maximize, self.steps = weight_decay, maximize, 0
+        self.m_scale = self.v_scale = None
+        if bits == 8:
+            self.m = [torch.zeros_like(p, dtype=torch.int8) for p in self.params]
+            self.v = [torch.zeros_like(p, dtype=torch.uint8) for p in self.params]
+            self.m_scale, self.v_scale = ([torch.zeros(-(-p.numel() // ADAMW_BLOCK), dtype=torch.float32,
+                                                       device=p.device) for p in self.params] for _ in range(2))
+        else:
+            self.m, self.v = ([torch.zeros_like(p, dtype=_wide(p.dtype)) for p in self.params] for _ in range(2))
+
+    def step(self, grads, *, lr=None, stream=None):
+        """One step with one gradient a parameter (None: that parameter is left as it is)."""
+        adamw_step(self.params, grads, self.m, self.v, self.steps + 1, self.lr if lr is None else lr,
+                   betas=self.betas, eps=self.eps, weight_decay=self.weight_decay, maximize=self.maximize,
+                   m_scale=self.m_scale, v_scale=self.v_scale, stream=stream)
+        self.steps += 1
