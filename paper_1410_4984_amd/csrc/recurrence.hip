@@ -20,6 +20,17 @@
 // once, each thread joins its rows, the slices are joined in shared memory, and with the state
 // before the tile each thread goes through its rows again, in registers.
 //
+// Short calls: the workgroups of a slab of channels go through the tiles one after the other and
+// keep the state in registers (one launch).  Longer ones: a workgroup for each tile, joined by a
+// chain in the workspace.  A tile publishes its piece as soon as it has read its rows.  Tiles are
+// in groups of 16; the state before a tile is the state after the group before (which that
+// group's last tile publishes) joined with the pieces of the tiles before it in its own group, always
+// in that order, so the result does not depend on timing.  Every published word
+// carries its own validity (it differs from the all-ones pattern that a first kernel writes), so
+// no ordering between words is needed.  Tiles are handed out by a counter in the order of the
+// rows: a workgroup only waits for tiles with smaller numbers, whose workgroups run already, and
+// the first of them waits for none, so every wait ends.
+//
 // The gate: with s = e / (1 + e), e = exp(-|gate|), the smaller of a and 1 - a is s to full
 // relative precision, and h = base + s (other - base) with base the operand of the larger weight.
 // A long memory (1 - a of 1e-3) then keeps its digits, which a rounded a times h would lose
@@ -54,6 +65,78 @@ struct RecArgs {
     const A *h0;                 // gradient: the state before a sequence's first row
     A *fin;                      // state after a sequence: h_last, or dh0 (may be NULL)
     int64_t tiles;               // along the rows
+    // the chain, in the workspace: (a, b) of each tile and channel, the state after each group
+    unsigned long long *next;    // the next tile to hand out
+    A *pieces, *states;
+};
+
+constexpr int kGroup = 16;       // tiles of a group
+
+// Words that other workgroups wait for.  A value is never the all-ones pattern (a NaN), which
+// stands for "not yet".
+template <typename U>
+__device__ inline U peek(const U *p) {
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <typename U>
+__device__ inline void put(U *p, U v) {
+    __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <typename U>
+__device__ inline U await(const U *p, U v) {
+    while (v == ~U(0)) {
+        __builtin_amdgcn_s_sleep(1);
+        v = peek(p);
+    }
+    return v;
+}
+
+template <typename A> struct Word;
+template <> struct Word<float> {
+    using U = uint32_t;
+    __device__ static U of(float x) {
+        const U u = __float_as_uint(x);
+        return u == ~U(0) ? 0x7fc00000u : u;
+    }
+    __device__ static float from(U u) { return __uint_as_float(u); }
+};
+template <> struct Word<double> {
+    using U = unsigned long long;
+    __device__ static U of(double x) {
+        const U u = (U)__double_as_longlong(x);
+        return u == ~U(0) ? 0x7ff8000000000000ull : u;
+    }
+    __device__ static double from(U u) { return __longlong_as_double((long long)u); }
+};
+
+// A piece (a, b): one word of 64 bits in single precision, two in double.
+template <typename A> struct Pair;
+template <> struct Pair<float> {
+    unsigned long long w;
+    __device__ void read(const float *p) { w = peek((const unsigned long long *)p); }
+    __device__ void wait(const float *p) { w = await((const unsigned long long *)p, w); }
+    __device__ float a() const { return __uint_as_float(uint32_t(w)); }
+    __device__ float b() const { return __uint_as_float(uint32_t(w >> 32)); }
+    __device__ static void write(float *p, float a, float b) {
+        put((unsigned long long *)p, (unsigned long long)Word<float>::of(a) | (unsigned long long)Word<float>::of(b) << 32);
+    }
+};
+template <> struct Pair<double> {
+    unsigned long long u, v;
+    __device__ void read(const double *p) {
+        u = peek((const unsigned long long *)p);
+        v = peek((const unsigned long long *)p + 1);
+    }
+    __device__ void wait(const double *p) {
+        u = await((const unsigned long long *)p, u);
+        v = await((const unsigned long long *)p + 1, v);
+    }
+    __device__ double a() const { return Word<double>::from(u); }
+    __device__ double b() const { return Word<double>::from(v); }
+    __device__ static void write(double *p, double a, double b) {
+        put((unsigned long long *)p, Word<double>::of(a));
+        put((unsigned long long *)p + 1, Word<double>::of(b));
+    }
 };
 
 __device__ inline float gate_part(float ag) {
@@ -159,7 +242,46 @@ __device__ inline void copy_empty(const RecArgs<T> &a, int64_t b, int64_t c, int
     for (int v = 0; v < n; ++v) a.fin[b * a.D + c + v] = a.init ? a.init[b * a.D + c + v] : A(0);
 }
 
-template <typename T, bool GRAD, int W, int R>
+// Before the tiles of a chain: its words, its counter, and the empty sequences.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void rec_init_kernel(RecArgs<T> a) {
+    using A = typename Elem<T>::Acc;
+    using U = typename Word<A>::U;
+    const int64_t at = int64_t(blockIdx.x) * kThreads + threadIdx.x, all = int64_t(gridDim.x) * kThreads;
+    if (at == 0) *a.next = 0;
+    const int64_t words = (a.tiles * 2 + (a.tiles + kGroup - 1) / kGroup) * a.D;     // the states lie behind the pieces
+    for (int64_t i = at; i < words; i += all) ((U *)a.pieces)[i] = ~U(0);
+    if (!a.fin || !a.offsets) return;
+    for (int64_t b = at / 64; b < a.B; b += all / 64)
+        for (int64_t c = at % 64; c < a.D; c += 64) copy_empty(a, b, c, 1);
+}
+
+// The state before tile `tile` of channel c, given by the chain.
+template <typename A>
+__device__ inline A chain_state(const A *pieces, const A *states, int64_t tile, int64_t D, int64_t c) {
+    using U = typename Word<A>::U;
+    const int64_t group = tile / kGroup;
+    const int before = int(tile % kGroup);
+    const U *sp = (const U *)states + (group - 1) * D + c;
+    const A *pp = pieces + (group * kGroup * D + c) * 2;
+    U w = 0;
+    if (group) w = peek(sp);
+    Pair<A> q[kGroup - 1];
+#pragma unroll
+    for (int j = 0; j < kGroup - 1; ++j)
+        if (j < before) q[j].read(pp + j * D * 2);
+    A state = 0;
+    if (group) state = Word<A>::from(await(sp, w));
+#pragma unroll
+    for (int j = 0; j < kGroup - 1; ++j)
+        if (j < before) {
+            q[j].wait(pp + j * D * 2);
+            state = after(state, q[j].a(), q[j].b());
+        }
+    return state;
+}
+
+template <typename T, bool GRAD, bool CHAIN, int W, int R>
 __global__ __launch_bounds__(kThreads) void rec_kernel(RecArgs<T> a) {
     using E = Elem<T>;
     using A = typename E::Acc;
@@ -168,13 +290,26 @@ __global__ __launch_bounds__(kThreads) void rec_kernel(RecArgs<T> a) {
     constexpr int V = E::V, kSlices = kThreads / W, kRows = kSlices * R, kCols = W * V;
     __shared__ int begins[kRows], ends[kRows], found;
     __shared__ A piece_a[kSlices][kCols], piece_b[kSlices][kCols], state[kCols];
+    __shared__ int64_t ticket;
     const int slice = threadIdx.x / W, lane = threadIdx.x % W;
-    const int64_t c0 = int64_t(blockIdx.x) * kCols, c = c0 + lane * V;
-    const int n = int(a.D - c < V ? (a.D > c ? a.D - c : 0) : V);
-    if (a.fin)
+    const int64_t slabs = (a.D + kCols - 1) / kCols;
+    int64_t tile = 0, c0 = int64_t(blockIdx.x) * kCols;
+    if (!CHAIN && a.fin) {
+        const int64_t c = c0 + lane * V;
+        const int n = int(a.D - c < V ? (a.D > c ? a.D - c : 0) : V);
         for (int64_t b = slice; b < a.B; b += kSlices) copy_empty(a, b, c, n);
+    }
     A carry = 0;                 // of channel c0 + threadIdx.x, in the first kCols threads
-    for (int64_t tile = 0; tile < a.tiles; ++tile) {
+    for (;; ++tile) {
+        if (CHAIN) {
+            if (threadIdx.x == 0) ticket = (int64_t)atomicAdd(a.next, 1ull);
+            __syncthreads();
+            tile = ticket / slabs;
+            c0 = ticket % slabs * kCols;
+        }
+        if (tile >= a.tiles) break;
+        const int64_t c = c0 + lane * V;
+        const int n = int(a.D - c < V ? (a.D > c ? a.D - c : 0) : V);
         const int64_t p0 = tile * kRows;
         const int len = int(a.N - p0 < kRows ? a.N - p0 : kRows);
         // rows of this thread: its part of the tile's, in order
@@ -225,8 +360,17 @@ __global__ __launch_bounds__(kThreads) void rec_kernel(RecArgs<T> a) {
                 piece_b[i][threadIdx.x] = tb;
                 join(ta, tb, na, nb);
             }
-            state[threadIdx.x] = carry;
-            carry = after(carry, ta, tb);
+            const int64_t ch = c0 + threadIdx.x;
+            if (!CHAIN) {
+                state[threadIdx.x] = carry;
+                carry = after(carry, ta, tb);
+            } else if (ch < a.D) {
+                Pair<A>::write(a.pieces + (tile * a.D + ch) * 2, ta, tb);
+                const A y = chain_state(a.pieces, a.states, tile, a.D, ch);
+                state[threadIdx.x] = y;
+                if (tile % kGroup == kGroup - 1)
+                    put((typename Word<A>::U *)a.states + tile / kGroup * a.D + ch, Word<A>::of(after(y, ta, tb)));
+            }
         }
         __syncthreads();
         A y[V];
@@ -270,20 +414,53 @@ __global__ __launch_bounds__(kThreads) void rec_kernel(RecArgs<T> a) {
 }
 
 constexpr int kLanes = 16;       // W: 256 bytes of a row
+constexpr int kSlicesOf = kThreads / kLanes;
 constexpr int kRowsMany = 16, kRowsFew = 4;
 
+// How a call is cut: rows of a thread, tiles along the rows, and whether they are chained.
+struct Cut {
+    int rows;
+    int64_t tiles;
+    bool chain;
+};
+
+Cut cut(int64_t N, int64_t D, int V) {
+    const int64_t slabs = (D + kLanes * V - 1) / (kLanes * V);
+    const int64_t few = kSlicesOf * kRowsFew, many = kSlicesOf * kRowsMany;
+    if (N <= 2 * few) return Cut{kRowsFew, (N + few - 1) / few, false};
+    if ((N + many - 1) / many * slabs < 512) return Cut{kRowsFew, (N + few - 1) / few, true};
+    return Cut{kRowsMany, (N + many - 1) / many, true};
+}
+
+constexpr size_t kCounterBytes = 256;
+
 template <typename T, bool GRAD>
-hipError_t launch(RecArgs<T> a, hipStream_t st) {
-    constexpr int kCols = kLanes * Elem<T>::V, kSlices = kThreads / kLanes;
+hipError_t launch(RecArgs<T> a, void *ws, hipStream_t st) {
+    using A = typename Elem<T>::Acc;
+    constexpr int kCols = kLanes * Elem<T>::V;
     const int64_t slabs = (a.D + kCols - 1) / kCols;
-    gpps::TimedScope ts(st, GRAD ? "recurrence_grad" : "recurrence_fwd");
-    if (a.N <= kSlices * kRowsFew) {
-        a.tiles = a.N > 0;
-        rec_kernel<T, GRAD, kLanes, kRowsFew><<<unsigned(slabs), kThreads, 0, st>>>(a);
-    } else {
-        a.tiles = (a.N + kSlices * kRowsMany - 1) / (kSlices * kRowsMany);
-        rec_kernel<T, GRAD, kLanes, kRowsMany><<<unsigned(slabs), kThreads, 0, st>>>(a);
+    const Cut k = cut(a.N, a.D, Elem<T>::V);
+    a.tiles = k.tiles;
+    if (!k.chain) {
+        gpps::TimedScope ts(st, GRAD ? "recurrence_grad" : "recurrence_fwd");
+        rec_kernel<T, GRAD, false, kLanes, kRowsFew><<<unsigned(slabs), kThreads, 0, st>>>(a);
+        return hipGetLastError();
     }
+    a.next = static_cast<unsigned long long *>(ws);
+    a.pieces = reinterpret_cast<A *>(static_cast<char *>(ws) + kCounterBytes);
+    a.states = a.pieces + 2 * a.tiles * a.D;
+    {
+        gpps::TimedScope ts(st, "recurrence_init");
+        const int64_t words = 3 * a.tiles * a.D;
+        rec_init_kernel<T><<<unsigned(std::min<int64_t>((words + kThreads * 8 - 1) / (kThreads * 8), 2048)), kThreads, 0, st>>>(a);
+        if (const hipError_t e = hipGetLastError()) return e;
+    }
+    gpps::TimedScope ts(st, GRAD ? "recurrence_grad" : "recurrence_fwd");
+    const unsigned blocks = unsigned(std::min<int64_t>(a.tiles * slabs, gpps::kMaxBlocks));
+    if (k.rows == kRowsFew)
+        rec_kernel<T, GRAD, true, kLanes, kRowsFew><<<blocks, kThreads, 0, st>>>(a);
+    else
+        rec_kernel<T, GRAD, true, kLanes, kRowsMany><<<blocks, kThreads, 0, st>>>(a);
     return hipGetLastError();
 }
 
@@ -319,7 +496,7 @@ void rows(const void *p, int64_t N, int64_t ld, bool down, S *&first, int64_t &s
 template <typename T>
 hipError_t forward(int64_t N, int64_t B, int64_t D, const void *x, int64_t ldx, const void *gate, int64_t ldg,
                    const int64_t *offsets, const void *h0, void *h, int64_t ldh, void *h_last, bool reverse,
-                   hipStream_t st) {
+                   void *ws, hipStream_t st) {
     using A = typename Elem<T>::Acc;
     RecArgs<T> a{};
     a.N = N, a.D = D, a.B = B, a.offsets = offsets, a.down = reverse;
@@ -327,14 +504,14 @@ hipError_t forward(int64_t N, int64_t B, int64_t D, const void *x, int64_t ldx, 
     rows(gate, N, ldg, reverse, a.gate, a.sgate);
     rows(h, N, ldh, reverse, a.out, a.sout);
     a.init = (const A *)h0, a.fin = (A *)h_last;
-    return launch<T, false>(a, st);
+    return launch<T, false>(a, ws, st);
 }
 
 template <typename T>
 hipError_t gradient(int64_t N, int64_t B, int64_t D, const void *x, int64_t ldx, const void *gate, int64_t ldg,
                     const void *h, int64_t ldh, const void *dh, int64_t lddh, const int64_t *offsets,
                     const void *h0, const void *dh_last, void *dx, int64_t lddx, void *dgate, int64_t lddg,
-                    void *dh0, bool reverse, hipStream_t st) {
+                    void *dh0, bool reverse, void *ws, hipStream_t st) {
     using A = typename Elem<T>::Acc;
     RecArgs<T> a{};
     const bool down = !reverse;  // the gradient runs against the recurrence
@@ -346,7 +523,7 @@ hipError_t gradient(int64_t N, int64_t B, int64_t D, const void *x, int64_t ldx,
     rows(dx, N, lddx, down, a.out, a.sout);
     rows(dgate, N, lddg, down, a.dgate, a.sdgate);
     a.init = (const A *)dh_last, a.h0 = (const A *)h0, a.fin = (A *)dh0;
-    return launch<T, true>(a, st);
+    return launch<T, true>(a, ws, st);
 }
 
 }  // namespace
@@ -355,7 +532,10 @@ extern "C" {
 
 size_t gpps_recurrence_workspace_bytes(gpps_dtype dt, int64_t N, int64_t B, int64_t D) {
     if (!valid_dtype(dt) || !valid_shape(N, B, D)) return 0;
-    return 256;
+    const Cut k = cut(N, D, int(16 / elem_size(dt)));
+    if (!k.chain) return kCounterBytes;
+    const int64_t words = (2 * k.tiles + (k.tiles + kGroup - 1) / kGroup) * D;
+    return gpps::align_up(kCounterBytes + size_t(words) * acc_size(dt), 256);
 }
 
 gpps_status gpps_recurrence(gpps_dtype dt, int64_t N, int64_t B, int64_t D, const void *x, int64_t ldx,
@@ -372,9 +552,9 @@ gpps_status gpps_recurrence(gpps_dtype dt, int64_t N, int64_t B, int64_t D, cons
     hipStream_t st = static_cast<hipStream_t>(stream);
     const bool rev = flags & GPPS_REVERSE;
     const hipError_t e =
-        dt == GPPS_F32   ? forward<float>(N, B, D, x, ldx, gate, ldg, offsets, h0, h, ldh, h_last, rev, st)
-        : dt == GPPS_F64 ? forward<double>(N, B, D, x, ldx, gate, ldg, offsets, h0, h, ldh, h_last, rev, st)
-                         : forward<bf16_t>(N, B, D, x, ldx, gate, ldg, offsets, h0, h, ldh, h_last, rev, st);
+        dt == GPPS_F32   ? forward<float>(N, B, D, x, ldx, gate, ldg, offsets, h0, h, ldh, h_last, rev, workspace, st)
+        : dt == GPPS_F64 ? forward<double>(N, B, D, x, ldx, gate, ldg, offsets, h0, h, ldh, h_last, rev, workspace, st)
+                         : forward<bf16_t>(N, B, D, x, ldx, gate, ldg, offsets, h0, h, ldh, h_last, rev, workspace, st);
     return e == hipSuccess ? GPPS_OK : GPPS_ERR_HIP;
 }
 
@@ -394,12 +574,12 @@ gpps_status gpps_recurrence_grads(gpps_dtype dt, int64_t N, int64_t B, int64_t D
     const bool rev = flags & GPPS_REVERSE;
     const hipError_t e =
         dt == GPPS_F32 ? gradient<float>(N, B, D, x, ldx, gate, ldg, h, ldh, dh, lddh, offsets, h0, dh_last, dx,
-                                         lddx, dgate, lddg, dh0, rev, st)
+                                         lddx, dgate, lddg, dh0, rev, workspace, st)
         : dt == GPPS_F64
             ? gradient<double>(N, B, D, x, ldx, gate, ldg, h, ldh, dh, lddh, offsets, h0, dh_last, dx, lddx, dgate,
-                               lddg, dh0, rev, st)
+                               lddg, dh0, rev, workspace, st)
             : gradient<bf16_t>(N, B, D, x, ldx, gate, ldg, h, ldh, dh, lddh, offsets, h0, dh_last, dx, lddx, dgate,
-                               lddg, dh0, rev, st);
+                               lddg, dh0, rev, workspace, st);
     return e == hipSuccess ? GPPS_OK : GPPS_ERR_HIP;
 }
 
