@@ -15,26 +15,31 @@
 // piece stays as it is.  It is a selection and not a product with zero, so that infinities and
 // NaN of one sequence never reach the next.
 //
-// A workgroup takes a tile of rows and channels: a thread holds R rows of 16 bytes (V
-// channels), S = 256 / W slices of R rows lie one after the other in time.  The tile is read
-// once, each thread joins its rows, the slices are joined in shared memory, and with the state
-// before the tile each thread goes through its rows again, in registers.
+// A workgroup takes a tile of rows and channels: a thread holds R rows of V channels, 16 bytes of
+// each, and slices of R rows lie one after the other in time.  The tile is read once: each thread
+// joins its rows, the slices are joined in shared memory, and with the state before the tile each
+// thread goes through its rows again, in registers, where the gates' sigmoids are kept.  A row's
+// last vector is moved back to end with the row where the width is no multiple of V: channels
+// don't mix, so the two threads that share some write the same values.
 //
-// Short calls: the workgroups of a slab of channels go through the tiles one after the other and
-// keep the state in registers (one launch).  Longer ones: a workgroup for each tile, joined by a
-// chain in the workspace.  A tile publishes its piece as soon as it has read its rows.  Tiles are
-// in groups of 16; the state before a tile is the state after the group before (which that
-// group's last tile publishes) joined with the pieces of the tiles before it in its own group, always
-// in that order, so the result does not depend on timing.  Every published word
-// carries its own validity (it differs from the all-ones pattern that a first kernel writes), so
-// no ordering between words is needed.  Tiles are handed out by a counter in the order of the
-// rows: a workgroup only waits for tiles with smaller numbers, whose workgroups run already, and
-// the first of them waits for none, so every wait ends.
+// Short calls: a workgroup goes through the tiles of its channels one after the other and keeps
+// the state in registers (one launch).  Longer ones: a workgroup for each tile, joined through
+// words in the workspace.  A tile publishes its piece as soon as it has read its rows; 16 tiles
+// make a group, whose last tile publishes the group's piece, and 16 groups a span, whose last
+// tile publishes the state after it.  The state before a tile is then that of the span before,
+// joined with the pieces of the groups before it in its span and of the tiles before it in
+// its group, always in that order, so the result does not depend on timing.  Where a tile's or
+// group's piece begins a sequence, nothing before it is waited for (its A = -1 would select
+// away what came: the same bits).  Every published word carries its own validity (it differs from
+// the all-ones pattern that a first kernel writes), so no ordering between words is needed.  Tiles
+// are handed out by a counter in the order of the rows: a workgroup only waits for tiles with
+// smaller numbers, whose workgroups run already, and the first of them waits for none, so
+// every wait ends.
 //
 // The gate: with s = e / (1 + e), e = exp(-|gate|), the smaller of a and 1 - a is s to full
 // relative precision, and h = base + s (other - base) with base the operand of the larger weight.
 // A long memory (1 - a of 1e-3) then keeps its digits, which a rounded a times h would lose
-// row by row.
+// row by row.  A thread keeps s with the gate's sign.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -46,8 +51,6 @@ namespace {
 
 using gpps::bf16_t;
 using gpps::Elem;
-
-constexpr int kThreads = 256;
 
 template <typename T>
 struct RecArgs {
@@ -64,13 +67,14 @@ struct RecArgs {
     const A *init;               // state before a sequence: h0, or dh_last (NULL: zero)
     const A *h0;                 // gradient: the state before a sequence's first row
     A *fin;                      // state after a sequence: h_last, or dh0 (may be NULL)
-    int64_t tiles;               // along the rows
-    // the chain, in the workspace: (a, b) of each tile and channel, the state after each group
-    unsigned long long *next;    // the next tile to hand out
-    A *pieces, *states;
+    int tiles;                   // along the rows
+    // the chain, in the workspace: (a, b) of each tile and channel, and of each group, and the state
+    // after each span
+    unsigned *next;              // the next tile to hand out
+    A *pieces, *groups, *states;
 };
 
-constexpr int kGroup = 16;       // tiles of a group
+constexpr int kGroup = 16;       // tiles of a group, and groups of a span
 
 // Words that other workgroups wait for.  A value is never the all-ones pattern (a NaN), which
 // stands for "not yet".
@@ -139,36 +143,50 @@ template <> struct Pair<double> {
     }
 };
 
-__device__ inline float gate_part(float ag) {
-    // exp(-|gate|): the product with log2(e) in two parts, so that it keeps its digits
+// e^-x for x >= 0.  Beside fp32 rows the product with log2(e) is taken in two parts, so that s is
+// good to the last bits; beside bfloat16 ones its own rounding (x 2^-24 relative) is far below the
+// gate's.
+template <bool FINE>
+__device__ inline float exp_minus(float x) {
     const float log2e = 1.44269504f, rest = 1.92596299e-8f;
-    const float t = -ag * log2e;
-    const float lo = ag < 128.0f ? __builtin_fmaf(-ag, log2e, -t) - ag * rest : 0.0f;
-    float e = __builtin_amdgcn_exp2f(t);
+    const float t = -x * log2e;
+    const float e = __builtin_amdgcn_exp2f(t);
+    if (!FINE) return e;
+    const float lo = x < 128.0f ? __builtin_fmaf(-x, log2e, -t) - x * rest : 0.0f;
     return __builtin_fmaf(e, lo * 0.693147181f, e);
 }
-__device__ inline double gate_part(double ag) { return exp(-ag); }
+template <bool FINE>
+__device__ inline double exp_minus(double x) { return exp(-x); }
 
 __device__ inline float reciprocal(float x) { return __builtin_amdgcn_rcpf(x); }
 __device__ inline double reciprocal(double x) { return 1.0 / x; }
 
-// s = min(a, 1 - a) and r = max(a, 1 - a).
-template <typename A>
-__device__ inline void gate_of(A g, A &s, A &r) {
-    const A e = gate_part(g < A(0) ? -g : g);
-    r = reciprocal(A(1) + e);
-    s = e * r;
-}
+__device__ inline bool negative(float x) { return __float_as_int(x) < 0; }
+__device__ inline bool negative(double x) { return __double_as_longlong(x) < 0; }
 
-template <typename A>
-__device__ inline A mix(A g, A s, A h, A x) {
-    const A base = g >= A(0) ? h : x, other = g >= A(0) ? x : h;
-    return base + s * (other - base);
+// min(a, 1 - a), with the gate's sign: negative where a is the smaller.
+template <bool FINE, typename A>
+__device__ inline A gate_of(A g) {
+    const A e = exp_minus<FINE>(g < A(0) ? -g : g);
+    return __builtin_elementwise_copysign(e * reciprocal(A(1) + e), g);
 }
-// a times y
 template <typename A>
-__device__ inline A times_gate(A g, A s, A y) {
-    return g >= A(0) ? y - s * y : s * y;
+__device__ inline A fmadd(A x, A y, A z) {
+    return __builtin_elementwise_fma(x, y, z);
+}
+// a h + (1 - a) x
+template <typename A>
+__device__ inline A mix(A t, A h, A x) {
+    return fmadd(t, x - h, negative(t) ? x : h);
+}
+// a y, and (1 - a) y
+template <typename A>
+__device__ inline A times_a(A t, A y) {
+    return fmadd(-t, y, negative(t) ? A(0) : y);
+}
+template <typename A>
+__device__ inline A times_b(A t, A y) {
+    return fmadd(t, y, negative(t) ? y : A(0));
 }
 
 // The piece (a1, b1) followed by (a2, b2), into the first.
@@ -186,7 +204,7 @@ __device__ inline A after(A state, A a, A b) {
 // Marks, for the positions p0 .. p0 + len - 1 of a tile, which sequence begins or ends there (-1:
 // none).  Called by all threads; ends with a barrier.  Offsets that break the contract change
 // which rows are marked, never what is accessed.
-template <int TR, typename T>
+template <int kThreads, int TR, typename T>
 __device__ inline void mark(const RecArgs<T> &a, int64_t p0, int len, int *begins, int *ends, int *found) {
     for (int i = threadIdx.x; i < TR; i += kThreads) begins[i] = ends[i] = -1;
     __syncthreads();
@@ -233,116 +251,150 @@ __device__ inline void mark(const RecArgs<T> &a, int64_t p0, int len, int *begin
     __syncthreads();
 }
 
-// Empty sequences hand their state on as it is.
+// Empty sequences hand their state on as it is: channel c of sequence b.
 template <typename T>
-__device__ inline void copy_empty(const RecArgs<T> &a, int64_t b, int64_t c, int n) {
+__device__ inline void copy_empty(const RecArgs<T> &a, int64_t b, int64_t c) {
     using A = typename Elem<T>::Acc;
     const int64_t o = a.offsets ? a.offsets[b] : 0, e = a.offsets ? a.offsets[b + 1] : a.N;
     if (e > o) return;
-    for (int v = 0; v < n; ++v) a.fin[b * a.D + c + v] = a.init ? a.init[b * a.D + c + v] : A(0);
+    a.fin[b * a.D + c] = a.init ? a.init[b * a.D + c] : A(0);
 }
 
-// Before the tiles of a chain: its words, its counter, and the empty sequences.
+__host__ __device__ inline int64_t groups_in(int64_t n) { return (n + kGroup - 1) / kGroup; }
+
+// Before the tiles of a chain: its words (pieces, groups, states, one behind the other), its
+// counter, and the empty sequences.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void rec_init_kernel(RecArgs<T> a) {
+__global__ __launch_bounds__(256) void rec_init_kernel(RecArgs<T> a) {
     using A = typename Elem<T>::Acc;
     using U = typename Word<A>::U;
-    const int64_t at = int64_t(blockIdx.x) * kThreads + threadIdx.x, all = int64_t(gridDim.x) * kThreads;
+    const int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x, all = int64_t(gridDim.x) * 256;
     if (at == 0) *a.next = 0;
-    const int64_t words = (a.tiles * 2 + (a.tiles + kGroup - 1) / kGroup) * a.D;     // the states lie behind the pieces
+    const int64_t groups = groups_in(a.tiles), words = (2 * a.tiles + 2 * groups + groups_in(groups)) * a.D;
     for (int64_t i = at; i < words; i += all) ((U *)a.pieces)[i] = ~U(0);
     if (!a.fin || !a.offsets) return;
     for (int64_t b = at / 64; b < a.B; b += all / 64)
-        for (int64_t c = at % 64; c < a.D; c += 64) copy_empty(a, b, c, 1);
+        for (int64_t c = at % 64; c < a.D; c += 64) copy_empty(a, b, c);
 }
 
-// The state before tile `tile` of channel c, given by the chain.
+// Joins the `n` published pieces at p, D apart, into (ta, tb), the last ones first read.
 template <typename A>
-__device__ inline A chain_state(const A *pieces, const A *states, int64_t tile, int64_t D, int64_t c) {
-    using U = typename Word<A>::U;
-    const int64_t group = tile / kGroup;
-    const int before = int(tile % kGroup);
-    const U *sp = (const U *)states + (group - 1) * D + c;
-    const A *pp = pieces + (group * kGroup * D + c) * 2;
-    U w = 0;
-    if (group) w = peek(sp);
+__device__ inline void join_published(const A *p, int n, int64_t D, A &ta, A &tb) {
     Pair<A> q[kGroup - 1];
 #pragma unroll
     for (int j = 0; j < kGroup - 1; ++j)
-        if (j < before) q[j].read(pp + j * D * 2);
-    A state = 0;
-    if (group) state = Word<A>::from(await(sp, w));
+        if (j < n) q[j].read(p + j * D * 2);
 #pragma unroll
     for (int j = 0; j < kGroup - 1; ++j)
-        if (j < before) {
-            q[j].wait(pp + j * D * 2);
-            state = after(state, q[j].a(), q[j].b());
+        if (j < n) {
+            q[j].wait(p + j * D * 2);
+            join(ta, tb, q[j].a(), q[j].b());
         }
+}
+
+// Publishes the piece (ta, tb) of tile `tile`, channel c, and whatever it is the last part of, and
+// returns the state before the tile.
+template <typename T, typename A>
+__device__ inline A chain(const RecArgs<T> &a, int tile, int64_t c, A ta, A tb) {
+    using U = typename Word<A>::U;
+    const int group = tile / kGroup, span = group / kGroup, tiles_before = tile % kGroup, groups_before = group % kGroup;
+    Pair<A>::write(a.pieces + (tile * a.D + c) * 2, ta, tb);
+    A pa = 1, pb = 0;                                        // the tiles before it in its group
+    join_published(a.pieces + (int64_t(group) * kGroup * a.D + c) * 2, tiles_before, a.D, pa, pb);
+    const bool ends_group = tiles_before == kGroup - 1;
+    if (ends_group) {
+        A ga = pa, gb = pb;
+        join(ga, gb, ta, tb);
+        Pair<A>::write(a.groups + (group * a.D + c) * 2, ga, gb);
+    }
+    A state = 0;
+    if (!(pa < A(0))) {
+        A qa = 1, qb = 0;
+        join_published(a.groups + (int64_t(span) * kGroup * a.D + c) * 2, groups_before, a.D, qa, qb);
+        if (span && !(qa < A(0))) {
+            const U *w = (const U *)a.states + (span - 1) * a.D + c;
+            state = Word<A>::from(await(w, peek(w)));
+        }
+        state = after(state, qa, qb);
+    }
+    state = after(state, pa, pb);
+    if (ends_group && groups_before == kGroup - 1)
+        put((U *)a.states + span * a.D + c, Word<A>::of(after(state, ta, tb)));
     return state;
 }
 
-template <typename T, bool GRAD, bool CHAIN, int W, int R>
-__global__ __launch_bounds__(kThreads) void rec_kernel(RecArgs<T> a) {
+// V of the N-wide array of accumulators at p, or zeros.
+template <typename A, int V>
+__device__ inline typename gpps::Wide<A, V>::type row_of(const A *p, int64_t at) {
+    using W = typename gpps::Wide<A, V>::type;
+    return p ? *reinterpret_cast<const W *>(p + at) : W(0);
+}
+
+template <typename T, int V, bool GRAD, bool CHAIN, int TH, int W, int R>
+__global__ __launch_bounds__(TH) void rec_kernel(RecArgs<T> a) {
     using E = Elem<T>;
     using A = typename E::Acc;
     using S = typename E::Store;
-    using Vec = typename gpps::Wide<S, E::V>::type;
-    constexpr int V = E::V, kSlices = kThreads / W, kRows = kSlices * R, kCols = W * V;
+    using Vec = typename gpps::Wide<S, V>::type;
+    using AVec = typename gpps::Wide<A, V>::type;
+    constexpr bool kFine = sizeof(S) == sizeof(A);
+    constexpr int kSlices = TH / W, kRows = kSlices * R, kCols = W * V;
+    static_assert(kSlices % 8 == 0 && kCols <= TH, "joins take eight slices at a time, a thread a column");
     __shared__ int begins[kRows], ends[kRows], found;
     __shared__ A piece_a[kSlices][kCols], piece_b[kSlices][kCols], state[kCols];
-    __shared__ int64_t ticket;
+    __shared__ unsigned ticket;
     const int slice = threadIdx.x / W, lane = threadIdx.x % W;
-    const int64_t slabs = (a.D + kCols - 1) / kCols;
-    int64_t tile = 0, c0 = int64_t(blockIdx.x) * kCols;
-    if (!CHAIN && a.fin) {
-        const int64_t c = c0 + lane * V;
-        const int n = int(a.D - c < V ? (a.D > c ? a.D - c : 0) : V);
-        for (int64_t b = slice; b < a.B; b += kSlices) copy_empty(a, b, c, n);
-    }
-    A carry = 0;                 // of channel c0 + threadIdx.x, in the first kCols threads
+    const unsigned slabs = unsigned((a.D + kCols - 1) / kCols);
+    int tile = 0;
+    int64_t c0 = int64_t(blockIdx.x) * kCols;
+    if (!CHAIN && a.fin)
+        for (int64_t b = slice; b < a.B; b += kSlices)
+            for (int64_t c = c0 + lane; c < c0 + kCols && c < a.D; c += W) copy_empty(a, b, c);
+    A carry = 0;                 // of column threadIdx.x
     for (;; ++tile) {
         if (CHAIN) {
-            if (threadIdx.x == 0) ticket = (int64_t)atomicAdd(a.next, 1ull);
+            if (threadIdx.x == 0) ticket = atomicAdd(a.next, 1u);
             __syncthreads();
-            tile = ticket / slabs;
-            c0 = ticket % slabs * kCols;
+            tile = int(ticket / slabs);
+            c0 = int64_t(ticket % slabs) * kCols;
         }
         if (tile >= a.tiles) break;
-        const int64_t c = c0 + lane * V;
-        const int n = int(a.D - c < V ? (a.D > c ? a.D - c : 0) : V);
-        const int64_t p0 = tile * kRows;
-        const int len = int(a.N - p0 < kRows ? a.N - p0 : kRows);
-        // rows of this thread: its part of the tile's, in order
-        const int i0 = slice * R;
-        const int64_t p = p0 + i0;
+        // this thread's channels, the last ones of the row where they would pass its end (threads
+        // wholly past it compute the same and store nothing), and its rows
+        const bool mine = c0 + lane * V < a.D;
+        const int64_t c = c0 + lane * V + V <= a.D ? c0 + lane * V : a.D - V;
+        const int64_t p0 = int64_t(tile) * kRows;
+        const int len = int(a.N - p0 < kRows ? a.N - p0 : kRows), i0 = slice * R;
         Vec gr[R], ur[R];        // gate, and what it weighs: x, or dh
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const int m = i0 + r < len ? n : 0;
-            gr[r] = gpps::load_some<S, V>(a.gate + (p + r) * a.sgate + c, m);
-            if (!GRAD) ur[r] = gpps::load_some<S, V>(a.x + (p + r) * a.sx + c, m);
-            else if (a.dh) ur[r] = gpps::load_some<S, V>(a.dh + (p + r) * a.sdh + c, m);
+            const int64_t p = p0 + (i0 + r < len ? i0 + r : len - 1);
+            gr[r] = *reinterpret_cast<const Vec *>(a.gate + p * a.sgate + c);
+            if (!GRAD) ur[r] = *reinterpret_cast<const Vec *>(a.x + p * a.sx + c);
+            else if (a.dh) ur[r] = *reinterpret_cast<const Vec *>(a.dh + p * a.sdh + c);
             else ur[r] = 0;
         }
-        mark<kRows>(a, p0, len, begins, ends, &found);
-        A pa[V], pb[V];
+        mark<TH, kRows>(a, p0, len, begins, ends, &found);
+        A t[R][V], pa[V], pb[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) pa[v] = 1, pb[v] = 0;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            if (i0 + r >= len) continue;
-            const int q = begins[i0 + r];
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const A g = E::up(gr[r][v]), u = E::up(ur[r][v]);
-                A s, rr;
-                gate_of(g, s, rr);
+            for (int v = 0; v < V; ++v) t[r][v] = gate_of<kFine>(E::up(gr[r][v]));
+            if (i0 + r < len) {
+                const int q = begins[i0 + r];
                 if (q >= 0) {
-                    pb[v] = a.init && v < n ? a.init[q * a.D + c + v] : A(0);
-                    pa[v] = -1;
+                    const AVec h0 = row_of<A, V>(a.init, q * a.D + c);
+#pragma unroll
+                    for (int v = 0; v < V; ++v) pb[v] = h0[v], pa[v] = -1;
                 }
-                pb[v] = GRAD ? times_gate(g, s, u + pb[v]) : mix(g, s, pb[v], u);
-                pa[v] = pa[v] < A(0) ? pa[v] : times_gate(g, s, pa[v]);
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const A u = E::up(ur[r][v]);
+                    pb[v] = GRAD ? times_a(t[r][v], u + pb[v]) : mix(t[r][v], pb[v], u);
+                    pa[v] = pa[v] < A(0) ? pa[v] : times_a(t[r][v], pa[v]);
+                }
             }
         }
 #pragma unroll
@@ -351,25 +403,39 @@ __global__ __launch_bounds__(kThreads) void rec_kernel(RecArgs<T> a) {
             piece_b[slice][lane * V + v] = pb[v];
         }
         __syncthreads();
+        Vec xr[GRAD ? R : 1], hr[GRAD ? R : 1];
+        if (GRAD) {
+            // the rows that only the outputs need, on their way while the state is waited for: x, and
+            // h of the row before in the recurrence, which is the next position's
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const int64_t p = p0 + (i0 + r < len ? i0 + r : len - 1), p1 = p + 1 < a.N ? p + 1 : p;
+                xr[r] = *reinterpret_cast<const Vec *>(a.x + p * a.sx + c);
+                hr[r] = *reinterpret_cast<const Vec *>(a.h + p1 * a.sh + c);
+            }
+        }
         if (threadIdx.x < kCols) {
             // each slice gets the piece before it within the tile
             A ta = 1, tb = 0;
-            for (int i = 0; i < kSlices; ++i) {
-                const A na = piece_a[i][threadIdx.x], nb = piece_b[i][threadIdx.x];
-                piece_a[i][threadIdx.x] = ta;
-                piece_b[i][threadIdx.x] = tb;
-                join(ta, tb, na, nb);
+            for (int i = 0; i < kSlices; i += 8) {
+                A na[8], nb[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) na[j] = piece_a[i + j][threadIdx.x], nb[j] = piece_b[i + j][threadIdx.x];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    piece_a[i + j][threadIdx.x] = ta;
+                    piece_b[i + j][threadIdx.x] = tb;
+                    join(ta, tb, na[j], nb[j]);
+                }
             }
-            const int64_t ch = c0 + threadIdx.x;
-            if (!CHAIN) {
+            if (CHAIN) {
+                // the channel of this column, by the rule above
+                const int64_t first = c0 + threadIdx.x / V * V;
+                const int64_t ch = (first + V <= a.D ? first : a.D - V) + threadIdx.x % V;
+                if (first < a.D) state[threadIdx.x] = chain(a, tile, ch, ta, tb);
+            } else {
                 state[threadIdx.x] = carry;
                 carry = after(carry, ta, tb);
-            } else if (ch < a.D) {
-                Pair<A>::write(a.pieces + (tile * a.D + ch) * 2, ta, tb);
-                const A y = chain_state(a.pieces, a.states, tile, a.D, ch);
-                state[threadIdx.x] = y;
-                if (tile % kGroup == kGroup - 1)
-                    put((typename Word<A>::U *)a.states + tile / kGroup * a.D + ch, Word<A>::of(after(y, ta, tb)));
             }
         }
         __syncthreads();
@@ -380,88 +446,109 @@ __global__ __launch_bounds__(kThreads) void rec_kernel(RecArgs<T> a) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const int i = i0 + r;
-            if (i >= len) continue;
-            const int q = begins[i], z = ends[i];
-            Vec o1, o2, xr, hr;
-            if (GRAD) {
-                xr = gpps::load_some<S, V>(a.x + (p + r) * a.sx + c, n);
-                hr = gpps::load_some<S, V>(a.h + (p + r + 1) * a.sh + c, z >= 0 || p + r + 1 >= a.N ? 0 : n);
-            }
+            if (i < len && mine) {
+                const int64_t p = p0 + i;
+                const int q = begins[i], z = ends[i];
+                if (q >= 0) {
+                    const AVec h0 = row_of<A, V>(a.init, q * a.D + c);
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const A g = E::up(gr[r][v]), u = E::up(ur[r][v]);
-                A s, rr;
-                gate_of(g, s, rr);
-                if (q >= 0) y[v] = a.init && v < n ? a.init[q * a.D + c + v] : A(0);
-                if (!GRAD) {
-                    y[v] = mix(g, s, y[v], u);
-                    o1[v] = E::down(y[v]);
-                } else {
-                    const A G = u + y[v];
-                    A before = E::up(hr[v]);
-                    if (z >= 0) before = a.h0 && v < n ? a.h0[z * a.D + c + v] : A(0);
-                    o1[v] = E::down((g >= A(0) ? s : rr) * G);
-                    o2[v] = E::down(s * rr * G * (before - E::up(xr[v])));
-                    y[v] = times_gate(g, s, G);
+                    for (int v = 0; v < V; ++v) y[v] = h0[v];
                 }
-                if (z >= 0 && a.fin && v < n) a.fin[z * a.D + c + v] = y[v];
+                Vec o1;
+                if (!GRAD) {
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        y[v] = mix(t[r][v], y[v], E::up(ur[r][v]));
+                        o1[v] = E::down(y[v]);
+                    }
+                } else {
+                    Vec o2;
+                    AVec before;
+#pragma unroll
+                    for (int v = 0; v < V; ++v) before[v] = E::up(hr[r][v]);
+                    if (z >= 0) before = row_of<A, V>(a.h0, z * a.D + c);
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        const A G = E::up(ur[r][v]) + y[v], dx = times_b(t[r][v], G);
+                        o1[v] = E::down(dx);
+                        o2[v] = E::down(times_a(t[r][v], dx) * (before[v] - E::up(xr[r][v])));
+                        y[v] = times_a(t[r][v], G);
+                    }
+                    *reinterpret_cast<Vec *>(a.dgate + p * a.sdgate + c) = o2;
+                }
+                *reinterpret_cast<Vec *>(a.out + p * a.sout + c) = o1;
+                if (z >= 0 && a.fin) {
+                    AVec last;
+#pragma unroll
+                    for (int v = 0; v < V; ++v) last[v] = y[v];
+                    *reinterpret_cast<AVec *>(a.fin + z * a.D + c) = last;
+                }
             }
-            gpps::store_some<S, V>(a.out + (p + r) * a.sout + c, n, o1);
-            if (GRAD) gpps::store_some<S, V>(a.dgate + (p + r) * a.sdgate + c, n, o2);
         }
         __syncthreads();         // the marks and pieces are written anew
     }
 }
 
 constexpr int kLanes = 16;       // W: 256 bytes of a row
-constexpr int kSlicesOf = kThreads / kLanes;
-constexpr int kRowsMany = 16, kRowsFew = 4;
+constexpr int kThreadsMany = 512, kRowsMany = 8, kThreadsFew = 256, kRowsFew = 4;
 
-// How a call is cut: rows of a thread, tiles along the rows, and whether they are chained.
+// How a call is cut: large tiles (256 rows) or small ones (64), how many along the rows, and whether
+// they are chained.
 struct Cut {
-    int rows;
+    bool large, chain;
     int64_t tiles;
-    bool chain;
 };
 
 Cut cut(int64_t N, int64_t D, int V) {
     const int64_t slabs = (D + kLanes * V - 1) / (kLanes * V);
-    const int64_t few = kSlicesOf * kRowsFew, many = kSlicesOf * kRowsMany;
-    if (N <= 2 * few) return Cut{kRowsFew, (N + few - 1) / few, false};
-    if ((N + many - 1) / many * slabs < 512) return Cut{kRowsFew, (N + few - 1) / few, true};
-    return Cut{kRowsMany, (N + many - 1) / many, true};
+    const int64_t few = kThreadsFew / kLanes * kRowsFew, many = kThreadsMany / kLanes * kRowsMany;
+    if (N <= 2 * few) return Cut{false, false, (N + few - 1) / few};
+    if ((N + many - 1) / many * slabs < 512) return Cut{false, true, (N + few - 1) / few};
+    return Cut{true, true, (N + many - 1) / many};
+}
+
+// Channels of a thread: 16 bytes, or one where a row has less.
+int vector_of(gpps_dtype dt, int64_t D) {
+    const int V = dt == GPPS_F64 ? 2 : dt == GPPS_BF16 ? 8 : 4;
+    return D < V ? 1 : V;
 }
 
 constexpr size_t kCounterBytes = 256;
 
-template <typename T, bool GRAD>
+template <typename T, int V, bool GRAD>
 hipError_t launch(RecArgs<T> a, void *ws, hipStream_t st) {
     using A = typename Elem<T>::Acc;
-    constexpr int kCols = kLanes * Elem<T>::V;
+    constexpr int kCols = kLanes * V;
     const int64_t slabs = (a.D + kCols - 1) / kCols;
-    const Cut k = cut(a.N, a.D, Elem<T>::V);
-    a.tiles = k.tiles;
+    const Cut k = cut(a.N, a.D, V);
+    a.tiles = int(k.tiles);
     if (!k.chain) {
         gpps::TimedScope ts(st, GRAD ? "recurrence_grad" : "recurrence_fwd");
-        rec_kernel<T, GRAD, false, kLanes, kRowsFew><<<unsigned(slabs), kThreads, 0, st>>>(a);
+        rec_kernel<T, V, GRAD, false, kThreadsFew, kLanes, kRowsFew><<<unsigned(slabs), kThreadsFew, 0, st>>>(a);
         return hipGetLastError();
     }
-    a.next = static_cast<unsigned long long *>(ws);
+    const int64_t groups = groups_in(k.tiles), words = (2 * k.tiles + 2 * groups + groups_in(groups)) * a.D;
+    a.next = static_cast<unsigned *>(ws);
     a.pieces = reinterpret_cast<A *>(static_cast<char *>(ws) + kCounterBytes);
-    a.states = a.pieces + 2 * a.tiles * a.D;
+    a.groups = a.pieces + 2 * k.tiles * a.D;
+    a.states = a.groups + 2 * groups * a.D;
     {
         gpps::TimedScope ts(st, "recurrence_init");
-        const int64_t words = 3 * a.tiles * a.D;
-        rec_init_kernel<T><<<unsigned(std::min<int64_t>((words + kThreads * 8 - 1) / (kThreads * 8), 2048)), kThreads, 0, st>>>(a);
+        rec_init_kernel<T><<<unsigned(std::min<int64_t>((words + 2047) / 2048, 2048)), 256, 0, st>>>(a);
         if (const hipError_t e = hipGetLastError()) return e;
     }
     gpps::TimedScope ts(st, GRAD ? "recurrence_grad" : "recurrence_fwd");
-    const unsigned blocks = unsigned(std::min<int64_t>(a.tiles * slabs, gpps::kMaxBlocks));
-    if (k.rows == kRowsFew)
-        rec_kernel<T, GRAD, true, kLanes, kRowsFew><<<blocks, kThreads, 0, st>>>(a);
+    const unsigned blocks = unsigned(std::min<int64_t>(k.tiles * slabs, gpps::kMaxBlocks / 2));
+    if (k.large)
+        rec_kernel<T, V, GRAD, true, kThreadsMany, kLanes, kRowsMany><<<blocks, kThreadsMany, 0, st>>>(a);
     else
-        rec_kernel<T, GRAD, true, kLanes, kRowsMany><<<blocks, kThreads, 0, st>>>(a);
+        rec_kernel<T, V, GRAD, true, kThreadsFew, kLanes, kRowsFew><<<blocks, kThreadsFew, 0, st>>>(a);
     return hipGetLastError();
+}
+
+template <typename T, bool GRAD>
+hipError_t launch(const RecArgs<T> &a, void *ws, hipStream_t st) {
+    return a.D < Elem<T>::V ? launch<T, 1, GRAD>(a, ws, st) : launch<T, Elem<T>::V, GRAD>(a, ws, st);
 }
 
 bool aligned(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
@@ -532,9 +619,9 @@ extern "C" {
 
 size_t gpps_recurrence_workspace_bytes(gpps_dtype dt, int64_t N, int64_t B, int64_t D) {
     if (!valid_dtype(dt) || !valid_shape(N, B, D)) return 0;
-    const Cut k = cut(N, D, int(16 / elem_size(dt)));
+    const Cut k = cut(N, D, vector_of(dt, D));
     if (!k.chain) return kCounterBytes;
-    const int64_t words = (2 * k.tiles + (k.tiles + kGroup - 1) / kGroup) * D;
+    const int64_t groups = groups_in(k.tiles), words = (2 * k.tiles + 2 * groups + groups_in(groups)) * D;
     return gpps::align_up(kCounterBytes + size_t(words) * acc_size(dt), 256);
 }
 
