@@ -167,7 +167,7 @@ __device__ inline bool negative(double x) { return __double_as_longlong(x) < 0; 
 // min(a, 1 - a), with the gate's sign: negative where a is the smaller.
 template <bool FINE, typename A>
 __device__ inline A gate_of(A g) {
-    const A e = exp_minus<FINE>(g < A(0) ? -g : g);
+    const A e = exp_minus<FINE>(__builtin_elementwise_abs(g));
     return __builtin_elementwise_copysign(e * reciprocal(A(1) + e), g);
 }
 template <typename A>
@@ -277,57 +277,37 @@ __global__ __launch_bounds__(256) void rec_init_kernel(RecArgs<T> a) {
         for (int64_t c = at % 64; c < a.D; c += 64) copy_empty(a, b, c);
 }
 
-// Joins the `n` published pieces at p, D apart, into (ta, tb), the last ones first read.
-template <typename A>
-__device__ inline void join_published(const A *p, int n, int64_t D, A &ta, A &tb) {
-    Pair<A> q[kGroup - 1];
+// This thread's share of joining `n` < kGroup published pieces of its column, D apart: helper h of
+// H takes up to ceil((kGroup - 1) / H) neighbouring ones.
+template <int H, typename A>
+__device__ inline void join_share(const A *p, int n, int64_t D, int h, A &ja, A &jb) {
+    constexpr int kEach = (kGroup - 1 + H - 1) / H;
+    Pair<A> q[kEach];
+    ja = 1, jb = 0;
 #pragma unroll
-    for (int j = 0; j < kGroup - 1; ++j)
-        if (j < n) q[j].read(p + j * D * 2);
+    for (int j = 0; j < kEach; ++j)
+        if (h * kEach + j < n) q[j].read(p + (h * kEach + j) * D * 2);
 #pragma unroll
-    for (int j = 0; j < kGroup - 1; ++j)
-        if (j < n) {
-            q[j].wait(p + j * D * 2);
-            join(ta, tb, q[j].a(), q[j].b());
+    for (int j = 0; j < kEach; ++j)
+        if (h * kEach + j < n) {
+            q[j].wait(p + (h * kEach + j) * D * 2);
+            join(ja, jb, q[j].a(), q[j].b());
         }
 }
 
-// Publishes the piece (ta, tb) of tile `tile`, channel c, and whatever it is the last part of, and
-// returns the state before the tile.
-template <typename T, typename A>
-__device__ inline A chain(const RecArgs<T> &a, int tile, int64_t c, A ta, A tb) {
-    using U = typename Word<A>::U;
-    const int group = tile / kGroup, span = group / kGroup, tiles_before = tile % kGroup, groups_before = group % kGroup;
-    Pair<A>::write(a.pieces + (tile * a.D + c) * 2, ta, tb);
-    A pa = 1, pb = 0;                                        // the tiles before it in its group
-    join_published(a.pieces + (int64_t(group) * kGroup * a.D + c) * 2, tiles_before, a.D, pa, pb);
-    const bool ends_group = tiles_before == kGroup - 1;
-    if (ends_group) {
-        A ga = pa, gb = pb;
-        join(ga, gb, ta, tb);
-        Pair<A>::write(a.groups + (group * a.D + c) * 2, ga, gb);
-    }
-    A state = 0;
-    if (!(pa < A(0))) {
-        A qa = 1, qb = 0;
-        join_published(a.groups + (int64_t(span) * kGroup * a.D + c) * 2, groups_before, a.D, qa, qb);
-        if (span && !(qa < A(0))) {
-            const U *w = (const U *)a.states + (span - 1) * a.D + c;
-            state = Word<A>::from(await(w, peek(w)));
-        }
-        state = after(state, qa, qb);
-    }
-    state = after(state, pa, pb);
-    if (ends_group && groups_before == kGroup - 1)
-        put((U *)a.states + span * a.D + c, Word<A>::of(after(state, ta, tb)));
-    return state;
-}
-
-// V of the N-wide array of accumulators at p, or zeros.
+// V neighbours of the array of accumulators at p (NULL: zeros).  Called where few rows need
+// them, in a branch: the empty statement makes the loads arrive there.  Otherwise every row would
+// wait, after the branch, for all memory operations on their way, its own stores among them.
 template <typename A, int V>
-__device__ inline typename gpps::Wide<A, V>::type row_of(const A *p, int64_t at) {
+__device__ inline void rare_row(const A *p, int64_t at, A (&y)[V]) {
     using W = typename gpps::Wide<A, V>::type;
-    return p ? *reinterpret_cast<const W *>(p + at) : W(0);
+    W w = 0;
+    if (p) w = *reinterpret_cast<const W *>(p + at);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        y[v] = w[v];
+        asm volatile("" : "+v"(y[v]));
+    }
 }
 
 template <typename T, int V, bool GRAD, bool CHAIN, int TH, int W, int R>
@@ -335,15 +315,18 @@ __global__ __launch_bounds__(TH) void rec_kernel(RecArgs<T> a) {
     using E = Elem<T>;
     using A = typename E::Acc;
     using S = typename E::Store;
+    using U = typename Word<A>::U;
     using Vec = typename gpps::Wide<S, V>::type;
     using AVec = typename gpps::Wide<A, V>::type;
     constexpr bool kFine = sizeof(S) == sizeof(A);
-    constexpr int kSlices = TH / W, kRows = kSlices * R, kCols = W * V;
-    static_assert(kSlices % 8 == 0 && kCols <= TH, "joins take eight slices at a time, a thread a column");
+    constexpr int kSlices = TH / W, kRows = kSlices * R, kCols = W * V, kHelp = CHAIN ? TH / kCols : 1;
+    static_assert(kSlices % 8 == 0 && TH % kCols == 0, "joins take eight slices at a time, threads a column");
     __shared__ int begins[kRows], ends[kRows], found;
     __shared__ A piece_a[kSlices][kCols], piece_b[kSlices][kCols], state[kCols];
+    __shared__ A share_a[CHAIN ? 2 : 1][kHelp][kCols], share_b[CHAIN ? 2 : 1][kHelp][kCols];
     __shared__ unsigned ticket;
     const int slice = threadIdx.x / W, lane = threadIdx.x % W;
+    const int column = threadIdx.x % kCols, helper = threadIdx.x / kCols;
     const unsigned slabs = unsigned((a.D + kCols - 1) / kCols);
     int tile = 0;
     int64_t c0 = int64_t(blockIdx.x) * kCols;
@@ -365,41 +348,49 @@ __global__ __launch_bounds__(TH) void rec_kernel(RecArgs<T> a) {
         const int64_t c = c0 + lane * V + V <= a.D ? c0 + lane * V : a.D - V;
         const int64_t p0 = int64_t(tile) * kRows;
         const int len = int(a.N - p0 < kRows ? a.N - p0 : kRows), i0 = slice * R;
+        const int rows = len - i0;                           // of this thread, if below R
+        const int64_t first = p0 + (rows > 0 ? i0 : 0);
         Vec gr[R], ur[R];        // gate, and what it weighs: x, or dh
+        {
+            const S *g = a.gate + first * a.sgate + c;
+            const int64_t su = GRAD ? a.sdh : a.sx;
+            const S *u = GRAD ? a.dh : a.x;
+            const bool some = !GRAD || u;
+            if (some) u += first * su + c;
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const int64_t p = p0 + (i0 + r < len ? i0 + r : len - 1);
-            gr[r] = *reinterpret_cast<const Vec *>(a.gate + p * a.sgate + c);
-            if (!GRAD) ur[r] = *reinterpret_cast<const Vec *>(a.x + p * a.sx + c);
-            else if (a.dh) ur[r] = *reinterpret_cast<const Vec *>(a.dh + p * a.sdh + c);
-            else ur[r] = 0;
+            for (int r = 0; r < R; ++r) {
+                gr[r] = *reinterpret_cast<const Vec *>(g);
+                ur[r] = 0;
+                if (some) ur[r] = *reinterpret_cast<const Vec *>(u);
+                if (r + 1 < rows) g += a.sgate, u += some ? su : 0;
+            }
         }
         mark<TH, kRows>(a, p0, len, begins, ends, &found);
         A t[R][V], pa[V], pb[V];
+        bool fresh = false;
 #pragma unroll
         for (int v = 0; v < V; ++v) pa[v] = 1, pb[v] = 0;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
 #pragma unroll
             for (int v = 0; v < V; ++v) t[r][v] = gate_of<kFine>(E::up(gr[r][v]));
-            if (i0 + r < len) {
+            if (r < rows) {
                 const int q = begins[i0 + r];
                 if (q >= 0) {
-                    const AVec h0 = row_of<A, V>(a.init, q * a.D + c);
-#pragma unroll
-                    for (int v = 0; v < V; ++v) pb[v] = h0[v], pa[v] = -1;
+                    fresh = true;
+                    rare_row(a.init, q * a.D + c, pb);
                 }
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
                     const A u = E::up(ur[r][v]);
                     pb[v] = GRAD ? times_a(t[r][v], u + pb[v]) : mix(t[r][v], pb[v], u);
-                    pa[v] = pa[v] < A(0) ? pa[v] : times_a(t[r][v], pa[v]);
+                    pa[v] = times_a(t[r][v], pa[v]);
                 }
             }
         }
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            piece_a[slice][lane * V + v] = pa[v];
+            piece_a[slice][lane * V + v] = fresh ? A(-1) : pa[v];
             piece_b[slice][lane * V + v] = pb[v];
         }
         __syncthreads();
@@ -407,81 +398,121 @@ __global__ __launch_bounds__(TH) void rec_kernel(RecArgs<T> a) {
         if (GRAD) {
             // the rows that only the outputs need, on their way while the state is waited for: x, and
             // h of the row before in the recurrence, which is the next position's
+            const S *x = a.x + first * a.sx + c, *h = a.h + (first + 1 < a.N ? first + 1 : first) * a.sh + c;
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                const int64_t p = p0 + (i0 + r < len ? i0 + r : len - 1), p1 = p + 1 < a.N ? p + 1 : p;
-                xr[r] = *reinterpret_cast<const Vec *>(a.x + p * a.sx + c);
-                hr[r] = *reinterpret_cast<const Vec *>(a.h + p1 * a.sh + c);
+                xr[r] = *reinterpret_cast<const Vec *>(x);
+                hr[r] = *reinterpret_cast<const Vec *>(h);
+                if (r + 1 < rows) x += a.sx;
+                if (r + 1 < rows && first + r + 2 < a.N) h += a.sh;
             }
         }
+        A ta = 1, tb = 0;        // the tile's piece
         if (threadIdx.x < kCols) {
             // each slice gets the piece before it within the tile
-            A ta = 1, tb = 0;
             for (int i = 0; i < kSlices; i += 8) {
                 A na[8], nb[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) na[j] = piece_a[i + j][threadIdx.x], nb[j] = piece_b[i + j][threadIdx.x];
+                for (int j = 0; j < 8; ++j) na[j] = piece_a[i + j][column], nb[j] = piece_b[i + j][column];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    piece_a[i + j][threadIdx.x] = ta;
-                    piece_b[i + j][threadIdx.x] = tb;
+                    piece_a[i + j][column] = ta;
+                    piece_b[i + j][column] = tb;
                     join(ta, tb, na[j], nb[j]);
                 }
             }
-            if (CHAIN) {
-                // the channel of this column, by the rule above
-                const int64_t first = c0 + threadIdx.x / V * V;
-                const int64_t ch = (first + V <= a.D ? first : a.D - V) + threadIdx.x % V;
-                if (first < a.D) state[threadIdx.x] = chain(a, tile, ch, ta, tb);
-            } else {
-                state[threadIdx.x] = carry;
-                carry = after(carry, ta, tb);
+        }
+        if (CHAIN) {
+            // the channel of this column, by the rule above
+            const int64_t lead = c0 + column / V * V;
+            const bool real = lead < a.D;
+            const int64_t ch = (lead + V <= a.D ? lead : a.D - V) + column % V;
+            const int group = tile / kGroup, span = group / kGroup;
+            const int tiles_before = tile % kGroup, groups_before = group % kGroup;
+            const bool ends_group = tiles_before == kGroup - 1;
+            if (threadIdx.x < kCols && real) Pair<A>::write(a.pieces + (tile * a.D + ch) * 2, ta, tb);
+            A pa = 1, pb = 0, ja, jb;                        // the tiles before it in its group
+            join_share<kHelp>(a.pieces + (int64_t(group) * kGroup * a.D + ch) * 2, tiles_before, a.D, helper, ja, jb);
+            share_a[0][helper][column] = ja;
+            share_b[0][helper][column] = jb;
+            __syncthreads();
+            for (int h = 0; h < kHelp; ++h) join(pa, pb, share_a[0][h][column], share_b[0][h][column]);
+            if (ends_group && threadIdx.x < kCols && real) {
+                A ga = pa, gb = pb;
+                join(ga, gb, ta, tb);
+                Pair<A>::write(a.groups + (group * a.D + ch) * 2, ga, gb);
             }
+            A y = 0;
+            if (group) {
+                const bool wait = !(pa < A(0));              // or a sequence begins in the group's part
+                join_share<kHelp>(a.groups + (int64_t(span) * kGroup * a.D + ch) * 2, wait ? groups_before : 0, a.D,
+                                  helper, ja, jb);
+                share_a[1][helper][column] = ja;
+                share_b[1][helper][column] = jb;
+                __syncthreads();
+                if (threadIdx.x < kCols && real) {
+                    A qa = 1, qb = 0;                        // the groups before it in its span
+                    for (int h = 0; h < kHelp; ++h) join(qa, qb, share_a[1][h][column], share_b[1][h][column]);
+                    if (span && wait && !(qa < A(0))) {
+                        const U *w = (const U *)a.states + (span - 1) * a.D + ch;
+                        y = Word<A>::from(await(w, peek(w)));
+                    }
+                    y = after(y, qa, qb);
+                }
+            }
+            if (threadIdx.x < kCols && real) {
+                y = after(y, pa, pb);
+                state[column] = y;
+                if (ends_group && groups_before == kGroup - 1)
+                    put((U *)a.states + span * a.D + ch, Word<A>::of(after(y, ta, tb)));
+            }
+        } else if (threadIdx.x < kCols) {
+            state[column] = carry;
+            carry = after(carry, ta, tb);
         }
         __syncthreads();
-        A y[V];
+        if (mine && rows > 0) {
+            A y[V];
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-            y[v] = after(state[lane * V + v], piece_a[slice][lane * V + v], piece_b[slice][lane * V + v]);
+            for (int v = 0; v < V; ++v)
+                y[v] = after(state[lane * V + v], piece_a[slice][lane * V + v], piece_b[slice][lane * V + v]);
+            S *out = a.out + first * a.sout + c, *dgate = GRAD ? a.dgate + first * a.sdgate + c : nullptr;
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const int i = i0 + r;
-            if (i < len && mine) {
-                const int64_t p = p0 + i;
-                const int q = begins[i], z = ends[i];
-                if (q >= 0) {
-                    const AVec h0 = row_of<A, V>(a.init, q * a.D + c);
+            for (int r = 0; r < R; ++r) {
+                if (r < rows) {
+                    const int q = begins[i0 + r], z = ends[i0 + r];
+                    if (q >= 0) rare_row(a.init, q * a.D + c, y);
+                    Vec o1;
+                    if (!GRAD) {
 #pragma unroll
-                    for (int v = 0; v < V; ++v) y[v] = h0[v];
-                }
-                Vec o1;
-                if (!GRAD) {
+                        for (int v = 0; v < V; ++v) {
+                            y[v] = mix(t[r][v], y[v], E::up(ur[r][v]));
+                            o1[v] = E::down(y[v]);
+                        }
+                    } else {
+                        Vec o2;
+                        A before[V];
 #pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        y[v] = mix(t[r][v], y[v], E::up(ur[r][v]));
-                        o1[v] = E::down(y[v]);
+                        for (int v = 0; v < V; ++v) before[v] = E::up(hr[r][v]);
+                        if (z >= 0) rare_row(a.h0, z * a.D + c, before);
+#pragma unroll
+                        for (int v = 0; v < V; ++v) {
+                            const A G = E::up(ur[r][v]) + y[v], dx = times_b(t[r][v], G);
+                            o1[v] = E::down(dx);
+                            o2[v] = E::down(times_a(t[r][v], dx) * (before[v] - E::up(xr[r][v])));
+                            y[v] = times_a(t[r][v], G);
+                        }
+                        *reinterpret_cast<Vec *>(dgate) = o2;
+                        dgate += a.sdgate;
                     }
-                } else {
-                    Vec o2;
-                    AVec before;
+                    *reinterpret_cast<Vec *>(out) = o1;
+                    out += a.sout;
+                    if (z >= 0 && a.fin) {
+                        AVec last;
 #pragma unroll
-                    for (int v = 0; v < V; ++v) before[v] = E::up(hr[r][v]);
-                    if (z >= 0) before = row_of<A, V>(a.h0, z * a.D + c);
-#pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        const A G = E::up(ur[r][v]) + y[v], dx = times_b(t[r][v], G);
-                        o1[v] = E::down(dx);
-                        o2[v] = E::down(times_a(t[r][v], dx) * (before[v] - E::up(xr[r][v])));
-                        y[v] = times_a(t[r][v], G);
+                        for (int v = 0; v < V; ++v) last[v] = y[v];
+                        *reinterpret_cast<AVec *>(a.fin + z * a.D + c) = last;
                     }
-                    *reinterpret_cast<Vec *>(a.dgate + p * a.sdgate + c) = o2;
-                }
-                *reinterpret_cast<Vec *>(a.out + p * a.sout + c) = o1;
-                if (z >= 0 && a.fin) {
-                    AVec last;
-#pragma unroll
-                    for (int v = 0; v < V; ++v) last[v] = y[v];
-                    *reinterpret_cast<AVec *>(a.fin + z * a.D + c) = last;
                 }
             }
         }
