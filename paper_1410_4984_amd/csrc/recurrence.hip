@@ -251,13 +251,14 @@ __device__ inline void mark(const RecArgs<T> &a, int64_t p0, int len, int *begin
     __syncthreads();
 }
 
-// Empty sequences hand their state on as it is: channel c of sequence b.
+// Empty sequences hand their state on as it is.
 template <typename T>
-__device__ inline void copy_empty(const RecArgs<T> &a, int64_t b, int64_t c) {
-    using A = typename Elem<T>::Acc;
-    const int64_t o = a.offsets ? a.offsets[b] : 0, e = a.offsets ? a.offsets[b + 1] : a.N;
-    if (e > o) return;
-    a.fin[b * a.D + c] = a.init ? a.init[b * a.D + c] : A(0);
+__device__ inline bool is_empty(const RecArgs<T> &a, int64_t b) {
+    return a.offsets ? a.offsets[b + 1] <= a.offsets[b] : a.N == 0;
+}
+template <typename T>
+__device__ inline void hand_on(const RecArgs<T> &a, int64_t b, int64_t c) {
+    a.fin[b * a.D + c] = a.init ? a.init[b * a.D + c] : typename Elem<T>::Acc(0);
 }
 
 __host__ __device__ inline int64_t groups_in(int64_t n) { return (n + kGroup - 1) / kGroup; }
@@ -274,7 +275,8 @@ __global__ __launch_bounds__(256) void rec_init_kernel(RecArgs<T> a) {
     for (int64_t i = at; i < words; i += all) ((U *)a.pieces)[i] = ~U(0);
     if (!a.fin || !a.offsets) return;
     for (int64_t b = at / 64; b < a.B; b += all / 64)
-        for (int64_t c = at % 64; c < a.D; c += 64) copy_empty(a, b, c);
+        if (is_empty(a, b))
+            for (int64_t c = at % 64; c < a.D; c += 64) hand_on(a, b, c);
 }
 
 // This thread's share of joining `n` < kGroup published pieces of its column, D apart: helper h of
@@ -311,7 +313,7 @@ __device__ inline void rare_row(const A *p, int64_t at, A (&y)[V]) {
 }
 
 template <typename T, int V, bool GRAD, bool CHAIN, int TH, int W, int R>
-__global__ __launch_bounds__(TH) void rec_kernel(RecArgs<T> a) {
+__global__ __launch_bounds__(TH) __attribute__((amdgpu_waves_per_eu(4))) void rec_kernel(RecArgs<T> a) {
     using E = Elem<T>;
     using A = typename E::Acc;
     using S = typename E::Store;
@@ -330,18 +332,27 @@ __global__ __launch_bounds__(TH) void rec_kernel(RecArgs<T> a) {
     const unsigned slabs = unsigned((a.D + kCols - 1) / kCols);
     int tile = 0;
     int64_t c0 = int64_t(blockIdx.x) * kCols;
-    if (!CHAIN && a.fin)
-        for (int64_t b = slice; b < a.B; b += kSlices)
-            for (int64_t c = c0 + lane; c < c0 + kCols && c < a.D; c += W) copy_empty(a, b, c);
-    A carry = 0;                 // of column threadIdx.x
-    for (;; ++tile) {
-        if (CHAIN) {
-            if (threadIdx.x == 0) ticket = atomicAdd(a.next, 1u);
-            __syncthreads();
-            tile = int(ticket / slabs);
-            c0 = int64_t(ticket % slabs) * kCols;
+    if (!CHAIN && a.fin) {
+        // four sequences at a time, so that their offsets are on their way together
+        for (int64_t b = slice; b < a.B; b += 4 * kSlices) {
+            bool none[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) none[j] = b + j * kSlices < a.B && is_empty(a, b + j * kSlices);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                for (int64_t c = c0 + lane; none[j] && c < c0 + kCols && c < a.D; c += W)
+                    hand_on(a, b + j * kSlices, c);
         }
-        if (tile >= a.tiles) break;
+    }
+    A carry = 0;                 // of column threadIdx.x
+    if (CHAIN) {
+        if (threadIdx.x == 0) ticket = atomicAdd(a.next, 1u);
+        __syncthreads();
+        tile = int(ticket / slabs);
+        c0 = int64_t(ticket % slabs) * kCols;
+    }
+    if (tile >= a.tiles) return;
+    do {
         // this thread's channels, the last ones of the row where they would pass its end (threads
         // wholly past it compute the same and store nothing), and its rows
         const bool mine = c0 + lane * V < a.D;
@@ -516,26 +527,35 @@ __global__ __launch_bounds__(TH) void rec_kernel(RecArgs<T> a) {
                 }
             }
         }
-        __syncthreads();         // the marks and pieces are written anew
-    }
+        if (!CHAIN) __syncthreads();         // the marks and pieces are written anew
+    } while (!CHAIN && ++tile < a.tiles);
 }
 
-constexpr int kLanes = 16;       // W: 256 bytes of a row
-constexpr int kThreadsMany = 512, kRowsMany = 8, kThreadsFew = 256, kRowsFew = 4;
+// Small tiles: 256 threads, 16 slices of 4 rows.  Large ones: 512 threads, 32 slices of 8 rows, or of 4
+// where a thread holds four arrays (the gradient: 131,072 x 1,024 fp32 580 us against 613 with 8
+// rows, of which half as many workgroups fit a CU) and where sequences are short: threads go to memory
+// for each sequence's first state one after the other (100,000 x 256 bf16, one row a sequence, 147 us
+// against 204, 25 rows 66 against 70; one sequence of 131,072 x 1,024 213 against 198).
+constexpr int kLanes = 16, kThreadsFew = 256, kThreadsMany = 512, kRowsFew = 4, kRowsMany = 8;
 
-// How a call is cut: large tiles (256 rows) or small ones (64), how many along the rows, and whether
-// they are chained.
+// How a call is cut: threads of a workgroup, rows of a thread, tiles along the rows, and whether they are
+// chained.
 struct Cut {
-    bool large, chain;
+    int threads, rows;
+    bool chain;
     int64_t tiles;
 };
 
-Cut cut(int64_t N, int64_t D, int V) {
+// Large tiles from the size on where they give every CU a workgroup (20,000 x 512 bf16, 316 of
+// them, 30.5 us against 39 in small tiles; 5,000 x 256 fp32, 80 of them, 22 against 21).  No chain for
+// one or two small tiles.
+Cut cut(int64_t N, int64_t B, int64_t D, int V, bool grad) {
     const int64_t slabs = (D + kLanes * V - 1) / (kLanes * V);
-    const int64_t few = kThreadsFew / kLanes * kRowsFew, many = kThreadsMany / kLanes * kRowsMany;
-    if (N <= 2 * few) return Cut{false, false, (N + few - 1) / few};
-    if ((N + many - 1) / many * slabs < 512) return Cut{false, true, (N + few - 1) / few};
-    return Cut{true, true, (N + many - 1) / many};
+    const int rows = grad || N < 32 * B ? kRowsFew : kRowsMany;
+    const int64_t few = kThreadsFew / kLanes * kRowsFew, many = kThreadsMany / kLanes * rows;
+    if (N <= 2 * few) return Cut{kThreadsFew, kRowsFew, false, (N + few - 1) / few};
+    if ((N + many - 1) / many * slabs < 256) return Cut{kThreadsFew, kRowsFew, true, (N + few - 1) / few};
+    return Cut{kThreadsMany, rows, true, (N + many - 1) / many};
 }
 
 // Channels of a thread: 16 bytes, or one where a row has less.
@@ -545,13 +565,13 @@ int vector_of(gpps_dtype dt, int64_t D) {
 }
 
 constexpr size_t kCounterBytes = 256;
+constexpr int64_t kMostTiles = 1 << 22;          // of one launch (its threads are counted in 32 bits)
 
 template <typename T, int V, bool GRAD>
 hipError_t launch(RecArgs<T> a, void *ws, hipStream_t st) {
     using A = typename Elem<T>::Acc;
-    constexpr int kCols = kLanes * V;
-    const int64_t slabs = (a.D + kCols - 1) / kCols;
-    const Cut k = cut(a.N, a.D, V);
+    const Cut k = cut(a.N, a.B, a.D, V, GRAD);
+    const int64_t slabs = (a.D + kLanes * V - 1) / (kLanes * V);
     a.tiles = int(k.tiles);
     if (!k.chain) {
         gpps::TimedScope ts(st, GRAD ? "recurrence_grad" : "recurrence_fwd");
@@ -569,12 +589,18 @@ hipError_t launch(RecArgs<T> a, void *ws, hipStream_t st) {
         if (const hipError_t e = hipGetLastError()) return e;
     }
     gpps::TimedScope ts(st, GRAD ? "recurrence_grad" : "recurrence_fwd");
-    const unsigned blocks = unsigned(std::min<int64_t>(k.tiles * slabs, gpps::kMaxBlocks / 2));
-    if (k.large)
-        rec_kernel<T, V, GRAD, true, kThreadsMany, kLanes, kRowsMany><<<blocks, kThreadsMany, 0, st>>>(a);
-    else
-        rec_kernel<T, V, GRAD, true, kThreadsFew, kLanes, kRowsFew><<<blocks, kThreadsFew, 0, st>>>(a);
-    return hipGetLastError();
+    // one workgroup a tile; the counter goes on over the launches of a call that needs several
+    for (int64_t left = k.tiles * slabs; left > 0; left -= kMostTiles) {
+        const unsigned blocks = unsigned(std::min(left, kMostTiles));
+        if (k.threads == kThreadsFew)
+            rec_kernel<T, V, GRAD, true, kThreadsFew, kLanes, kRowsFew><<<blocks, kThreadsFew, 0, st>>>(a);
+        else if (k.rows == kRowsFew)
+            rec_kernel<T, V, GRAD, true, kThreadsMany, kLanes, kRowsFew><<<blocks, kThreadsMany, 0, st>>>(a);
+        else if constexpr (!GRAD)
+            rec_kernel<T, V, false, true, kThreadsMany, kLanes, kRowsMany><<<blocks, kThreadsMany, 0, st>>>(a);
+        if (const hipError_t e = hipGetLastError()) return e;
+    }
+    return hipSuccess;
 }
 
 template <typename T, bool GRAD>
@@ -650,10 +676,14 @@ extern "C" {
 
 size_t gpps_recurrence_workspace_bytes(gpps_dtype dt, int64_t N, int64_t B, int64_t D) {
     if (!valid_dtype(dt) || !valid_shape(N, B, D)) return 0;
-    const Cut k = cut(N, D, vector_of(dt, D));
-    if (!k.chain) return kCounterBytes;
-    const int64_t groups = groups_in(k.tiles), words = (2 * k.tiles + 2 * groups + groups_in(groups)) * D;
-    return gpps::align_up(kCounterBytes + size_t(words) * acc_size(dt), 256);
+    // the larger of the two directions'
+    size_t bytes = 0;
+    for (bool grad : {false, true}) {
+        const Cut k = cut(N, B, D, vector_of(dt, D), grad);
+        const int64_t groups = groups_in(k.tiles), words = (2 * k.tiles + 2 * groups + groups_in(groups)) * D;
+        bytes = std::max(bytes, k.chain ? size_t(words) * acc_size(dt) : 0);
+    }
+    return gpps::align_up(kCounterBytes + bytes, 256);
 }
 
 gpps_status gpps_recurrence(gpps_dtype dt, int64_t N, int64_t B, int64_t D, const void *x, int64_t ldx,
