@@ -90,24 +90,27 @@ def _ld(x, name, dtype, shape, device) -> int:
     import torch
     if not isinstance(x, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
-    if x.device != device or x.dtype != dtype:
+    if x.dtype != dtype or x.device != device:
         raise ValueError(f"{name}: expected {dtype} on {device}, got {x.dtype} on {x.device}")
-    if tuple(x.shape) != shape:
+    if x.shape != shape:
         raise ValueError(f"{name}: expected shape {shape}, got {tuple(x.shape)}")
     N, D = shape
-    if (D > 1 and x.stride(1) != 1) or (N > 1 and x.stride(0) < D):
+    row, one = x.stride()
+    if (D > 1 and one != 1) or (N > 1 and row < D):
         raise ValueError(f"{name}: a row's elements must be neighbours and rows must not overlap "
                          f"(strides {x.stride()})")
-    return x.stride(0) if N > 1 else D
+    return row if N > 1 else D
 
 
 def _ptr(x):
     return None if x is None else x.data_ptr()
 
 
-def _current(device):
+def _current(device) -> int:
+    """The current stream's handle (what torch.cuda.current_stream(device).cuda_stream is, without
+    its 2 us)."""
     import torch
-    return torch.cuda.current_stream(device).cuda_stream
+    return torch._C._cuda_getCurrentRawStream(device.index)
 
 
 def _on_stream(stream, tensors, call):
@@ -154,8 +157,8 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, *, out=None, stream=None):
         _dev_tensor(bias, "bias", wide, (D,), device)
     if out is None:
         y = torch.empty((N, D), dtype=dtype, device=device)
-        stats = torch.empty((2, N), dtype=wide, device=device)
-        mean, rstd = stats[0], stats[1]
+        mean = torch.empty(N, dtype=wide, device=device)
+        rstd = torch.empty(N, dtype=wide, device=device)
         ldy = D
     else:
         y, mean, rstd = out
@@ -313,6 +316,17 @@ def _held(t, what, i, dtype, n, device):
     return t.data_ptr()
 
 
+def _all_held(ts, what, dtype, sizes, device):
+    """The addresses of a list's tensors, checked like _held (in passes over the list: a step of a small
+    network is mostly its tensors' checks)."""
+    k = len(ts)
+    if ([t.dtype for t in ts].count(dtype) != k or [t.device for t in ts].count(device) != k
+            or [t.numel() for t in ts] != sizes or not all([t.is_contiguous() for t in ts])):
+        for i, (t, n) in enumerate(zip(ts, sizes)):
+            _held(t, what, i, dtype, n, device)
+    return [t.data_ptr() for t in ts]
+
+
 def adamw_step(params, grads, m, v, step, lr, *, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01,
                maximize=False, m_scale=None, v_scale=None, stream=None):
     """One AdamW step over lists of tensors, in place.
@@ -339,48 +353,46 @@ def adamw_step(params, grads, m, v, step, lr, *, betas=(0.9, 0.999), eps=1e-8, w
     lists = (grads, m, v) + ((m_scale, v_scale) if eight else ())
     if any(len(l) != count for l in lists):
         raise ValueError("params, grads, m, v (and the scales) must be lists of one length")
-    groups = {}
-    device = None
-    for i in range(count):
-        p, g = params[i], grads[i]
-        if g is None:
-            continue
-        if device is None:
-            device = p.device
-            if device.type != "cuda":
-                raise ValueError(f"params[{i}] must be a GPU tensor (got {device})")
-            if device.index != torch.cuda.current_device():
-                raise ValueError(f"params[{i}] is on {device}, which is not the current device")
-        dtype, gtype, n = p.dtype, g.dtype, p.numel()
-        group = groups.get((dtype, gtype))
-        if group is None:
-            _row_dt(dtype)
-            if gtype != dtype and {dtype, gtype} != {torch.float32, torch.bfloat16}:
-                raise TypeError(f"grads[{i}]: {gtype} beside parameters of {dtype}")
-            if eight and dtype == torch.float64:
-                raise TypeError(f"params[{i}]: 8-bit moments are held beside float32 and bfloat16 parameters only")
-            group = groups[dtype, gtype] = ([], [], [], [], [], [], [])
-        wide = _wide(dtype)
-        group[0].append(n)
-        group[1].append(_held(p, "params", i, dtype, n, device))
-        group[2].append(_held(g, "grads", i, gtype, n, device))
-        group[3].append(_held(m[i], "m", i, torch.int8 if eight else wide, n, device))
-        group[4].append(_held(v[i], "v", i, torch.uint8 if eight else wide, n, device))
-        if eight:
-            blocks = -(-n // ADAMW_BLOCK)
-            group[5].append(_held(m_scale[i], "m_scale", i, torch.float32, blocks, device))
-            group[6].append(_held(v_scale[i], "v_scale", i, torch.float32, blocks, device))
-    if not groups:
+    some = [i for i in range(count) if grads[i] is not None]
+    if not some:
         return
-    for group in groups.values():
-        some = [q for q, n in zip(group[1], group[0]) if n]
-        if len(set(some)) < len(some):
-            raise ValueError("a tensor is listed twice")
+    if len(some) < count:
+        params, lists = [params[i] for i in some], [[l[i] for i in some] for l in lists]
+    device = params[0].device
+    if device.type != "cuda":
+        raise ValueError(f"params must be GPU tensors (got {device})")
+    if device.index != torch.cuda.current_device():
+        raise ValueError(f"params are on {device}, which is not the current device")
+    types = [(p.dtype, g.dtype) for p, g in zip(params, lists[0])]
+    calls, seen = [], []
+    for dtype, gtype in dict.fromkeys(types):
+        _row_dt(dtype)
+        if gtype != dtype and {dtype, gtype} != {torch.float32, torch.bfloat16}:
+            raise TypeError(f"gradients of {gtype} beside parameters of {dtype}")
+        if eight and dtype == torch.float64:
+            raise TypeError("8-bit moments are held beside float32 and bfloat16 parameters only")
+        mine = (params, *lists)
+        if types.count((dtype, gtype)) < len(types):
+            at = [i for i, t in enumerate(types) if t == (dtype, gtype)]
+            mine = [[l[i] for i in at] for l in mine]
+        sizes = [p.numel() for p in mine[0]]
+        wide = _wide(dtype)
+        held = [_all_held(mine[0], "params", dtype, sizes, device), _all_held(mine[1], "grads", gtype, sizes, device),
+                _all_held(mine[2], "m", torch.int8 if eight else wide, sizes, device),
+                _all_held(mine[3], "v", torch.uint8 if eight else wide, sizes, device)]
+        if eight:
+            blocks = [-(-n // ADAMW_BLOCK) for n in sizes]
+            held += [_all_held(mine[4], "m_scale", torch.float32, blocks, device),
+                     _all_held(mine[5], "v_scale", torch.float32, blocks, device)]
+        seen += [q for q, n in zip(held[0], sizes) if n]
+        calls.append((dtype, gtype, sizes, held))
+    if len(set(seen)) < len(seen):
+        raise ValueError("a tensor is listed twice")
     st = _current(device)
     L = _lib()
-    for (dtype, gtype), group in groups.items():
-        k = len(group[0])
-        arrays = [(ctypes.c_int64 * k)(*group[0])] + [(ctypes.c_void_p * k)(*a) if a else None for a in group[1:]]
+    for dtype, gtype, sizes, held in calls:
+        k = len(sizes)
+        arrays = [(ctypes.c_int64 * k)(*sizes)] + [(ctypes.c_void_p * k)(*a) for a in held] + [None] * (6 - len(held))
         bits = 8 if eight else 64 if dtype == torch.float64 else 32
         _check(L.gpps_adamw(_row_dt(dtype), _row_dt(gtype), bits, k, *arrays, int(step), float(lr), float(betas[0]),
                             float(betas[1]), float(eps), float(weight_decay), MAXIMIZE if maximize else 0, st))
