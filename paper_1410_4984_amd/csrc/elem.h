@@ -69,10 +69,29 @@ __device__ inline void store_some(S *p, int n, typename Wide<S, V>::type x) {
         if (v < n) p[v] = x[v];
 }
 
-// Sum over groups of `width` neighbouring lanes (a power of two), the same in each of them.
-template <typename A>
-__device__ inline A lanes_sum(A x, int width) {
-    for (int o = 1; o < width; o <<= 1) x += __shfl_xor(x, o);
+// x of the lane that the DPP control names.
+template <int CTRL>
+__device__ inline float lane_of(float x) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, false));
+}
+template <int CTRL>
+__device__ inline double lane_of(double x) {
+    const long long u = __double_as_longlong(x);
+    const int lo = __builtin_amdgcn_update_dpp(0, int(u), CTRL, 0xf, 0xf, false);
+    const int hi = __builtin_amdgcn_update_dpp(0, int(u >> 32), CTRL, 0xf, 0xf, false);
+    return __longlong_as_double((long long)hi << 32 | (unsigned)lo);
+}
+
+// Sum over groups of WIDTH neighbouring lanes (8, 16, 32 or 64), the same bits in each of them.
+// Within 16 lanes by DPP moves (the neighbour, the other pair, the other four, the other eight).
+template <int WIDTH, typename A>
+__device__ inline A lanes_sum(A x) {
+    x += lane_of<0xb1>(x);                   // quad_perm 1, 0, 3, 2
+    x += lane_of<0x4e>(x);                   // quad_perm 2, 3, 0, 1
+    x += lane_of<0x141>(x);                  // row_half_mirror
+    if constexpr (WIDTH >= 16) x += lane_of<0x140>(x);       // row_mirror
+    if constexpr (WIDTH >= 32) x += __shfl_xor(x, 16);
+    if constexpr (WIDTH >= 64) x += __shfl_xor(x, 32);
     return x;
 }
 
