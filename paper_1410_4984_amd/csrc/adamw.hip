@@ -7,8 +7,9 @@
 // Every element is touched once, so the step is bound by its bytes: 28 of them for fp32
 // parameters and gradients with 32-bit moments, 16 with 8-bit ones.  A launch takes up to 64
 // tensors, whose pointers travel in the kernel's arguments (no table to upload, so a call
-// needs no workspace and no copy): a workgroup takes 2,048 neighbouring elements of one
-// tensor, which it finds from the tensors' first workgroups by bisection.
+// needs no workspace and no copy): a workgroup takes 1,024 neighbouring elements of one
+// tensor (four a thread, once: 501 us for 100 million fp32 parameters, 518 with 2,048, 542 with 8,192),
+// which it finds from the tensors' first workgroups by bisection.
 //
 // 8-bit moments: the elements of a tensor in blocks of 256, each with two scales in fp32, the
 // block's largest |m| and largest v.  A code stands for
@@ -35,7 +36,7 @@ using gpps::Elem;
 using gpps::Wide;
 
 constexpr int kTensors = 64;     // of one launch: 3.9 KB of arguments
-constexpr int kChunk = 2048;     // elements of one workgroup
+constexpr int kChunk = 1024;     // elements of one workgroup
 constexpr int kBlock = GPPS_ADAMW_BLOCK;
 
 struct Tensor {
@@ -62,8 +63,12 @@ struct Coef {
     A sign;                      // -1: maximise
 };
 
-__device__ inline float root_of(float x) { return sqrtf(x); }
+// The step's root and quotient: in 32 bits by the hardware's approximations (one unit in the last place
+// each, of a step that is itself a small part of p), in 64 as they are.
+__device__ inline float root_of(float x) { return __builtin_amdgcn_sqrtf(x); }
 __device__ inline double root_of(double x) { return sqrt(x); }
+__device__ inline float quotient(float x, float y) { return x * __builtin_amdgcn_rcpf(y); }
+__device__ inline double quotient(double x, double y) { return x / y; }
 
 template <typename A>
 __device__ inline void moments(A g, A &m, A &v, const Coef<A> &c) {
@@ -74,7 +79,7 @@ __device__ inline void moments(A g, A &m, A &v, const Coef<A> &c) {
 
 template <typename A>
 __device__ inline A update(A p, A m, A v, const Coef<A> &c) {
-    return p * c.keep - m / (root_of(v) * c.root + c.eps) * c.step;
+    return p * c.keep - quotient(m, root_of(v) * c.root + c.eps) * c.step;
 }
 
 __device__ inline float value_m(int c, float s) {
@@ -90,14 +95,48 @@ __device__ inline float value_v(int c, float s) {
     return s * (r2 * r2);
 }
 
-// The largest of a wave's values, NaN if any of them is.
-__device__ inline float wave_max(float x) {
-    for (int o = 1; o < 64; o <<= 1) {
-        const float y = __shfl_xor(x, o);
-        x = (y > x || y != y) ? y : x;
+// Codes: rint(127 sqrt(x)) and rint(255 sqrt(sqrt(x))), roots and products rounded to nearest.  The
+// hardware's root is off by at most a unit in the last place, so the product by less than 6.1e-5 (of
+// up to 127) or 1.2e-4 (of up to 255, two roots): unless it lies so close to where two codes meet, its
+// code is that of the exact root.  About a wave in ten has a value that does, and takes the exact
+// roots, which the compiler writes as some fifteen instructions each (100 million fp32 parameters, their
+// moments read back: 548 us, with exact roots throughout 600).
+// (A NaN or infinite scale keeps the block's values non-finite; its codes are within bounds.)
+__device__ inline int bounded(float c, float top) { return int(fminf(fmaxf(c, 0.0f), top)); }
+
+__device__ inline void codes_of(const float (&x)[4], const float (&y)[4], int (&m)[4], int (&v)[4]) {
+#pragma clang fp contract(off)
+    float near_m = 0.0f, near_v = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float tm = __builtin_amdgcn_sqrtf(x[e]) * 127.0f, rm = rintf(tm);
+        const float tv = __builtin_amdgcn_sqrtf(__builtin_amdgcn_sqrtf(y[e])) * 255.0f, rv = rintf(tv);
+        near_m = fmaxf(near_m, fabsf(tm - rm));
+        near_v = fmaxf(near_v, fabsf(tv - rv));
+        m[e] = bounded(rm, 127.0f);
+        v[e] = bounded(rv, 255.0f);
     }
-    return x;
+    if (near_m > 0.5f - 6.1e-5f || near_v > 0.5f - 1.2e-4f)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            m[e] = bounded(rintf(sqrtf(x[e]) * 127.0f), 127.0f);
+            v[e] = bounded(rintf(sqrtf(sqrtf(y[e])) * 255.0f), 255.0f);
+        }
 }
+
+// The largest of a wave's values x >= 0, NaN if any of them is: as whole numbers their bits are in the same
+// order, and NaN's are above all others.
+__device__ inline float wave_max(unsigned x) {
+    auto step = [&](unsigned y) { x = y > x ? y : x; };
+    step(__builtin_amdgcn_update_dpp(0, int(x), 0xb1, 0xf, 0xf, false));      // quad_perm 1, 0, 3, 2
+    step(__builtin_amdgcn_update_dpp(0, int(x), 0x4e, 0xf, 0xf, false));      // quad_perm 2, 3, 0, 1
+    step(__builtin_amdgcn_update_dpp(0, int(x), 0x141, 0xf, 0xf, false));     // row_half_mirror
+    step(__builtin_amdgcn_update_dpp(0, int(x), 0x140, 0xf, 0xf, false));     // row_mirror
+    step(__shfl_xor(x, 16));
+    step(__shfl_xor(x, 32));
+    return __uint_as_float(x);
+}
+__device__ inline unsigned magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
 __device__ inline int tensor_of(const Batch &b, uint32_t block) {
     int lo = 0, hi = b.count - 1;
@@ -109,6 +148,16 @@ __device__ inline int tensor_of(const Batch &b, uint32_t block) {
     return lo;
 }
 
+// The part of a thread: four elements (n of them inside the tensor) from element i on.
+struct Place {
+    int64_t i;
+    int n;
+};
+__device__ inline Place place_of(const Batch &b, int k, int64_t size) {
+    const int64_t i = int64_t(blockIdx.x - b.first[k]) * kChunk + threadIdx.x * 4;
+    return Place{i, int(i >= size ? 0 : size - i < 4 ? size - i : 4)};
+}
+
 template <typename P, typename G>
 __global__ __launch_bounds__(256) void adamw_kernel(Batch b, Coef<typename Elem<P>::Acc> c) {
     using A = typename Elem<P>::Acc;
@@ -116,84 +165,70 @@ __global__ __launch_bounds__(256) void adamw_kernel(Batch b, Coef<typename Elem<
     using GS = typename Elem<G>::Store;
     const int k = tensor_of(b, blockIdx.x);
     const Tensor t = b.t[k];
-    const int64_t i0 = int64_t(blockIdx.x - b.first[k]) * kChunk;
-    const int64_t i1 = i0 + kChunk < t.n ? i0 + kChunk : t.n;
-    for (int64_t i = i0 + threadIdx.x * 4; i < i1; i += 256 * 4) {
-        const int n = int(i1 - i < 4 ? i1 - i : 4);
-        auto p = gpps::load_some<PS, 4>((const PS *)t.p + i, n);
-        const auto g = gpps::load_some<GS, 4>((const GS *)t.g + i, n);
-        auto m = gpps::load_some<A, 4>((const A *)t.m + i, n);
-        auto v = gpps::load_some<A, 4>((const A *)t.v + i, n);
+    const auto [i, n] = place_of(b, k, t.n);
+    auto p = gpps::load_some<PS, 4>((const PS *)t.p + i, n);
+    const auto g = gpps::load_some<GS, 4>((const GS *)t.g + i, n);
+    auto m = gpps::load_some<A, 4>((const A *)t.m + i, n);
+    auto v = gpps::load_some<A, 4>((const A *)t.v + i, n);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            A me = m[e], ve = v[e];
-            moments(A(Elem<G>::up(g[e])) * c.sign, me, ve, c);
-            p[e] = Elem<P>::down(update(A(Elem<P>::up(p[e])), me, ve, c));
-            m[e] = me;
-            v[e] = ve;
-        }
-        gpps::store_some<PS, 4>((PS *)t.p + i, n, p);
-        gpps::store_some<A, 4>((A *)t.m + i, n, m);
-        gpps::store_some<A, 4>((A *)t.v + i, n, v);
+    for (int e = 0; e < 4; ++e) {
+        A me = m[e], ve = v[e];
+        moments(A(Elem<G>::up(g[e])) * c.sign, me, ve, c);
+        p[e] = Elem<P>::down(update(A(Elem<P>::up(p[e])), me, ve, c));
+        m[e] = me;
+        v[e] = ve;
     }
+    gpps::store_some<PS, 4>((PS *)t.p + i, n, p);
+    gpps::store_some<A, 4>((A *)t.m + i, n, m);
+    gpps::store_some<A, 4>((A *)t.v + i, n, v);
 }
 
+// A wave takes one block of a scale.
 template <typename P, typename G>
 __global__ __launch_bounds__(256) void adamw8_kernel(Batch b, Coef<float> c) {
     using PS = typename Elem<P>::Store;
     using GS = typename Elem<G>::Store;
     const int k = tensor_of(b, blockIdx.x);
     const Tensor t = b.t[k];
-    const int64_t i0 = int64_t(blockIdx.x - b.first[k]) * kChunk;
-    const int64_t i1 = i0 + kChunk < t.n ? i0 + kChunk : t.n;
-    const int lane = threadIdx.x % 64;
-    for (int64_t i = i0 + threadIdx.x / 64 * kBlock; i < i1; i += 4 * kBlock) {
-        const int64_t at = i + lane * 4;
-        const int n = int(at >= i1 ? 0 : i1 - at < 4 ? i1 - at : 4);
-        auto p = gpps::load_some<PS, 4>((const PS *)t.p + at, n);
-        const auto g = gpps::load_some<GS, 4>((const GS *)t.g + at, n);
-        auto cm = gpps::load_some<int8_t, 4>((const int8_t *)t.m + at, n);
-        auto cv = gpps::load_some<uint8_t, 4>((const uint8_t *)t.v + at, n);
-        const float ms = t.ms[i / kBlock], vs = t.vs[i / kBlock];
-        float m[4], v[4], top_m = 0.0f, top_v = 0.0f;
+    const auto [i, n] = place_of(b, k, t.n);
+    auto p = gpps::load_some<PS, 4>((const PS *)t.p + i, n);
+    const auto g = gpps::load_some<GS, 4>((const GS *)t.g + i, n);
+    auto cm = gpps::load_some<int8_t, 4>((const int8_t *)t.m + i, n);
+    auto cv = gpps::load_some<uint8_t, 4>((const uint8_t *)t.v + i, n);
+    const float ms = n ? t.ms[i / kBlock] : 0.0f, vs = n ? t.vs[i / kBlock] : 0.0f;
+    float m[4], v[4];
+    unsigned most_m = 0, most_v = 0;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            m[e] = v[e] = 0.0f;
-            if (e < n) {
-                m[e] = value_m(cm[e], ms);
-                v[e] = value_v(cv[e], vs);
-                moments(Elem<G>::up(g[e]) * c.sign, m[e], v[e], c);
-                p[e] = Elem<P>::down(update(Elem<P>::up(p[e]), m[e], v[e], c));
-            }
-            const float am = fabsf(m[e]);
-            top_m = (am > top_m || am != am) ? am : top_m;
-            top_v = (v[e] > top_v || v[e] != v[e]) ? v[e] : top_v;
-        }
-        top_m = wave_max(top_m);
-        top_v = wave_max(top_v);
-        // scales below the normal range have no reciprocal: such a block's moment is zero
-        if (top_m < __FLT_MIN__) top_m = 0.0f;
-        if (top_v < __FLT_MIN__) top_v = 0.0f;
-        const float im = top_m > 0.0f ? 1.0f / top_m : 0.0f, iv = top_v > 0.0f ? 1.0f / top_v : 0.0f;
+    for (int e = 0; e < 4; ++e) {
+        // (past the tensor's end: zeros, that nothing keeps)
+        m[e] = value_m(cm[e], ms);
+        v[e] = value_v(cv[e], vs);
+        moments(Elem<G>::up(g[e]) * c.sign, m[e], v[e], c);
+        p[e] = Elem<P>::down(update(Elem<P>::up(p[e]), m[e], v[e], c));
+        most_m = max(most_m, magnitude(m[e]));
+        most_v = max(most_v, magnitude(v[e]));
+    }
+    float top_m = wave_max(most_m), top_v = wave_max(most_v);
+    // scales below the normal range have no reciprocal: such a block's moment is zero
+    if (top_m < __FLT_MIN__) top_m = 0.0f;
+    if (top_v < __FLT_MIN__) top_v = 0.0f;
+    const float im = top_m > 0.0f ? 1.0f / top_m : 0.0f, iv = top_v > 0.0f ? 1.0f / top_v : 0.0f;
+    float xm[4], xv[4];
+    int qm[4], qv[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-#pragma clang fp contract(off)
-            // (a NaN or infinite scale keeps the block's values non-finite; its codes are clamped)
-            const float um = rintf(sqrtf(fabsf(m[e]) * im) * 127.0f);
-            const float uv = rintf(sqrtf(sqrtf(v[e] * iv)) * 255.0f);
-            const int qm = int(fminf(fmaxf(um, 0.0f), 127.0f));
-            int qv = int(fminf(fmaxf(uv, 0.0f), 255.0f));
-            if (v[e] > 0.0f && top_v > 0.0f && qv < 1) qv = 1;
-            cm[e] = int8_t(m[e] < 0.0f ? -qm : qm);
-            cv[e] = uint8_t(qv);
-        }
-        gpps::store_some<PS, 4>((PS *)t.p + at, n, p);
-        gpps::store_some<int8_t, 4>((int8_t *)t.m + at, n, cm);
-        gpps::store_some<uint8_t, 4>((uint8_t *)t.v + at, n, cv);
-        if (lane == 0) {
-            t.ms[i / kBlock] = top_m;
-            t.vs[i / kBlock] = top_v;
-        }
+    for (int e = 0; e < 4; ++e) xm[e] = fabsf(m[e]) * im, xv[e] = v[e] * iv;
+    codes_of(xm, xv, qm, qv);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        cm[e] = int8_t(m[e] < 0.0f ? -qm[e] : qm[e]);
+        cv[e] = uint8_t(v[e] > 0.0f && top_v > 0.0f && qv[e] < 1 ? 1 : qv[e]);
+    }
+    gpps::store_some<PS, 4>((PS *)t.p + i, n, p);
+    gpps::store_some<int8_t, 4>((int8_t *)t.m + i, n, cm);
+    gpps::store_some<uint8_t, 4>((uint8_t *)t.v + i, n, cv);
+    if (threadIdx.x % 64 == 0 && n) {
+        t.ms[i / kBlock] = top_m;
+        t.vs[i / kBlock] = top_v;
     }
 }
 
@@ -209,7 +244,10 @@ __global__ __launch_bounds__(256) void adamw_values_kernel(int64_t n, const C *_
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             v[e] = sizeof(C) == 1 && C(-1) < C(0) ? value_m(c[e], s) : value_v(c[e], s);
-        gpps::store_some<float, 4>(out + i, k, v);
+        // (past the caches, where the codes of the next elements are: 550 us -> 527 for the step over 100 million
+        // parameters with both moments read back)
+        if (k == 4) __builtin_nontemporal_store(v, reinterpret_cast<Wide<float, 4>::type *>(out + i));
+        else gpps::store_some<float, 4>(out + i, k, v);
     }
 }
 
