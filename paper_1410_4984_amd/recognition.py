@@ -1,0 +1,206 @@
+"""Recognition model for the Bayesian GP-LVM: q(x_n) computed from the data.
+
+``gplvm.fit`` gives every row its own mu_n and S_n.  Here a network with shared
+weights computes them from Y, with memory along the rows of each sequence, so a
+fitted model gives the latent point of rows it has not seen in one pass, and the
+number of parameters does not grow with N:
+
+    a = layer_norm(Y W0 + b0)            [N x H]
+    (x, gate) = a W1 + b1                one pair per direction
+    h = recurrence(x, gate)              along each sequence, and against it unless causal
+    (m, s) = layer_norm(h) W2 + b2       [N x Q] each
+    mu = Y P + m,  S = exp(s)            P starts as the PCA projection
+
+The objective is the bound of ``gpps.bound`` (fp64), whose dmu and dS come back
+through the network by the operators' gradients; one AdamW step then updates every
+weight, Z and the logarithms of sigma_f2, l and beta.  The products with W0 .. W2
+are torch's.
+
+    fit(Y, Q, M, offsets=...) -> FitResult(model, bound_trace, ...)
+    model.infer(Y, offsets) -> (mu, S)
+    model.stream(y, state) -> (mu, S, state)     causal models: new rows of running sequences
+"""
+from __future__ import annotations
+
+import dataclasses
+import time
+
+import numpy as np
+
+from . import bound, bound_workspace_bytes
+from .operators import AdamW, layer_norm, layer_norm_grads, recurrence, recurrence_grads
+
+_NAMES = ("P", "W0", "b0", "g0", "c0", "W1", "b1", "g1", "c1", "W2", "b2")
+
+
+class Recognizer:
+    """The network: ``weights`` (a dict of tensors), the data's ``mean`` and ``scale``."""
+
+    def __init__(self, D: int, Q: int, hidden: int = 64, *, causal: bool = False, projection=None,
+                 mean=None, scale: float = 1.0, log_variance: float = -2.0, seed: int = 0, dtype=None,
+                 device: str = "cuda:0"):
+        import torch
+        dtype = torch.float32 if dtype is None else dtype
+        if dtype not in (torch.float32, torch.float64):
+            raise TypeError(f"unsupported dtype {dtype}")
+        self.D, self.Q, self.hidden, self.causal, self.dtype = D, Q, hidden, causal, dtype
+        ways = 1 if causal else 2
+        rng = np.random.default_rng(seed)
+
+        def tensor(a):
+            return torch.tensor(np.asarray(a, np.float64), dtype=dtype, device=device)
+
+        def matrix(rows, cols):
+            return tensor(rng.normal(size=(rows, cols)) / np.sqrt(rows))
+
+        H = hidden
+        b1 = np.zeros((ways, 2, H))
+        b1[:, 1] = rng.uniform(-1.0, 4.0, size=(ways, H))    # gates: memories of about one to fifty rows
+        b2 = np.concatenate([np.zeros(Q), np.full(Q, log_variance)])
+        self.weights = {
+            "P": tensor(np.zeros((D, Q)) if projection is None else projection),
+            "W0": matrix(D, H), "b0": tensor(np.zeros(H)), "g0": tensor(np.ones(H)), "c0": tensor(np.zeros(H)),
+            "W1": matrix(H, 2 * ways * H), "b1": tensor(b1.ravel()),
+            "g1": tensor(np.ones(ways * H)), "c1": tensor(np.zeros(ways * H)),
+            "W2": 0.1 * matrix(ways * H, 2 * Q), "b2": tensor(b2)}
+        self.mean = tensor(np.zeros(D) if mean is None else mean)
+        self.scale = float(scale)
+
+    def forward(self, Y, offsets=None, states=None):
+        """mu, log S and what ``backward`` needs, for scaled rows Y [N x D]."""
+        import torch
+        w, H = self.weights, self.hidden
+        N = Y.shape[0]
+        a0 = torch.addmm(w["b0"], Y, w["W0"])
+        n0, mean0, rstd0 = layer_norm(a0, w["g0"], w["c0"])
+        a1 = torch.addmm(w["b1"], n0, w["W1"])
+        ways = 1 if self.causal else 2
+        B = 1 if offsets is None else offsets.shape[0] - 1
+        h = torch.empty((N, ways * H), dtype=self.dtype, device=Y.device)
+        last = torch.empty((ways, B, H), dtype=self.dtype, device=Y.device)
+        for k in range(ways):
+            recurrence(a1[:, 2 * k * H:(2 * k + 1) * H], a1[:, (2 * k + 1) * H:(2 * k + 2) * H], offsets,
+                       states, reverse=k == 1, out=(h[:, k * H:(k + 1) * H], last[k]))
+        n1, mean1, rstd1 = layer_norm(h, w["g1"], w["c1"])
+        out = torch.addmm(w["b2"], n1, w["W2"])
+        mu = torch.addmm(out[:, :self.Q], Y, w["P"])
+        return mu, out[:, self.Q:], (Y, offsets, a0, n0, mean0, rstd0, a1, h, n1, mean1, rstd1), last[0]
+
+    def backward(self, kept, dmu, dlogS):
+        """Gradients of the weights (a dict) from those of mu and log S."""
+        import torch
+        Y, offsets, a0, n0, mean0, rstd0, a1, h, n1, mean1, rstd1 = kept
+        w, H = self.weights, self.hidden
+        dout = torch.cat([dmu, dlogS], 1)
+        g1 = layer_norm_grads(h, w["g1"], mean1, rstd1, dout @ w["W2"].t())
+        da1 = torch.empty_like(a1)
+        for k in range(1 if self.causal else 2):
+            part = slice(k * H, (k + 1) * H)
+            x, gate = slice(2 * k * H, (2 * k + 1) * H), slice((2 * k + 1) * H, (2 * k + 2) * H)
+            recurrence_grads(a1[:, x], a1[:, gate], h[:, part], g1["dx"][:, part], offsets, reverse=k == 1,
+                             out={"dx": da1[:, x], "dgate": da1[:, gate], "dh0": None})
+        g0 = layer_norm_grads(a0, w["g0"], mean0, rstd0, da1 @ w["W1"].t())
+        return {"P": Y.t() @ dmu, "W0": Y.t() @ g0["dx"], "b0": g0["dx"].sum(0), "g0": g0["dweight"],
+                "c0": g0["dbias"], "W1": n0.t() @ da1, "b1": da1.sum(0), "g1": g1["dweight"], "c1": g1["dbias"],
+                "W2": n1.t() @ dout, "b2": dout.sum(0)}
+
+    def _rows(self, Y):
+        import torch
+        Y = torch.as_tensor(Y).to(device=self.mean.device, dtype=self.dtype)
+        return ((Y - self.mean) / self.scale).contiguous()
+
+    def infer(self, Y, offsets=None):
+        """(mu, S) [N x Q] of the rows of Y (one sequence, or those that ``offsets`` marks)."""
+        mu, logS, _, _ = self.forward(self._rows(Y), _offsets(offsets, Y.shape[0], self.mean.device))
+        return mu, logS.exp()
+
+    def stream(self, y, state=None):
+        """One new row of each of B running sequences: y [B x D] and the state of the call before
+        (None: the sequences begin).  Returns (mu, S, state)."""
+        import torch
+        if not self.causal:
+            raise ValueError("stream needs a causal model: the other direction begins at a sequence's end")
+        offsets = torch.arange(y.shape[0] + 1, device=self.mean.device)
+        mu, logS, _, state = self.forward(self._rows(y), offsets, state)
+        return mu, logS.exp(), state
+
+
+def _offsets(offsets, N: int, device):
+    """Sequence bounds as the operators take them, checked on the host when they come from there."""
+    import torch
+    if offsets is None or isinstance(offsets, torch.Tensor) and offsets.device.type == "cuda":
+        return offsets
+    o = np.asarray(offsets, np.int64)
+    if o.ndim != 1 or o.size < 2 or o[0] != 0 or o[-1] != N or np.any(np.diff(o) < 0):
+        raise ValueError(f"offsets begin with 0, never fall and end with {N}")
+    return torch.tensor(o, device=device)
+
+
+@dataclasses.dataclass
+class FitResult:
+    model: Recognizer
+    Z: np.ndarray
+    sigma_f2: float
+    l: np.ndarray
+    beta: float
+    bound_trace: list        # L before every step
+    seconds: float
+
+
+def fit(Y: np.ndarray, Q: int, M: int, *, offsets=None, hidden: int = 64, causal: bool = False, steps: int = 500,
+        lr: float = 1e-2, bits: int = 32, weight_decay: float = 0.0, jitter: float = 1e-4, dtype=None, seed: int = 0,
+        device: str = "cuda:0") -> FitResult:
+    """Maximise the bound over the recognition weights, Z, sigma_f2, l and beta with AdamW.
+
+    Y [N x D]: rows of sequences, one after the other, with ``offsets`` [B + 1] their bounds (None: one
+    sequence).  The rows are centred and scaled to unit variance internally (sigma_f2 and beta are
+    those of the scaled rows).  lr falls to a twentieth along half a cosine.  ``bits``: how AdamW holds
+    the weights' moments (8 or 32; those of Z and the kernel parameters are in 64).  A step that leads
+    to a bound that is not finite (a matrix lost positive definiteness) is taken back, and the rate
+    halved."""
+    import torch
+
+    Y = np.asarray(Y, np.float64)
+    N, D = Y.shape
+    mean, scale = Y.mean(0), float(Y.std())
+    Ys = (Y - mean) / scale
+    _, sing, Vt = np.linalg.svd(Ys, full_matrices=False)
+    projection = Vt[:Q].T / (sing[:Q] / np.sqrt(N))          # PCA means of unit variance
+    model = Recognizer(D, Q, hidden, causal=causal, projection=projection, mean=mean, scale=scale, seed=seed,
+                       dtype=dtype, device=device)
+    rng = np.random.default_rng(seed)
+    Yt64 = torch.tensor(Ys, dtype=torch.float64, device=device)
+    Yt = Yt64.to(model.dtype)
+    off = _offsets(offsets, N, Yt.device)
+    Z = torch.tensor(Ys[rng.choice(N, size=M, replace=False)] @ projection, dtype=torch.float64, device=device)
+    logs = torch.zeros(Q + 2, dtype=torch.float64, device=device)    # log sigma_f2, log l, log beta
+    logs[-1] = np.log(10.0)
+    opt = AdamW([model.weights[k] for k in _NAMES], lr, weight_decay=weight_decay, bits=bits, maximize=True)
+    kernel_opt = AdamW([Z, logs], lr, weight_decay=0.0, maximize=True)
+    ws = torch.empty(bound_workspace_bytes(torch.float64, N, M, Q, D), dtype=torch.uint8, device=device)
+    everything = (*opt.params, Z, logs)
+    before = [t.clone() for t in everything]
+    out, trace, rate, t0 = None, [], 1.0, time.perf_counter()
+    for step in range(steps):
+        sf2, *l, beta = np.exp(logs.tolist())
+        mu, logS, kept, _ = model.forward(Yt, off)
+        S = logS.double().exp()
+        out = bound(mu.double(), S, Z, Yt64, sf2, l, beta, jitter, out=out, workspace=ws)
+        L = float(out["L"])
+        if not np.isfinite(L):
+            rate *= 0.5
+            if rate < 1e-3:
+                break
+            for t, k in zip(everything, before):             # to where the step that led here began
+                t.copy_(k)
+            continue
+        trace.append(L)
+        for t, k in zip(everything, before):
+            k.copy_(t)
+        grads = model.backward(kept, (out["dmu"] / N).to(model.dtype), (out["dS"] * S / N).to(model.dtype))
+        now = rate * lr * (0.05 + 0.475 * (1 + np.cos(np.pi * step / steps)))
+        opt.step([grads[k] for k in _NAMES], lr=now)
+        chain = torch.exp(logs)
+        kernel_opt.step([out["dZ"] / N, torch.cat([out["dsigma_f2"], out["dl"], out["dbeta"]]) * chain / N], lr=now)
+    sf2, *l, beta = np.exp(logs.tolist())
+    return FitResult(model, Z.cpu().numpy(), float(sf2), np.array(l), float(beta), trace, time.perf_counter() - t0)
