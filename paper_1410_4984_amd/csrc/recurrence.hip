@@ -321,7 +321,7 @@ __global__ __launch_bounds__(TH) __attribute__((amdgpu_waves_per_eu(4))) void re
     using Vec = typename gpps::Wide<S, V>::type;
     using AVec = typename gpps::Wide<A, V>::type;
     constexpr bool kFine = sizeof(S) == sizeof(A);
-    constexpr int kSlices = TH / W, kRows = kSlices * R, kCols = W * V, kHelp = CHAIN ? TH / kCols : 1;
+    constexpr int kSlices = TH / W, kRows = kSlices * R, kCols = W * V, kHelp = CHAIN ? (TH / kCols < 8 ? TH / kCols : 8) : 1;
     static_assert(kSlices % 8 == 0 && TH % kCols == 0, "joins take eight slices at a time, threads a column");
     __shared__ int begins[kRows], ends[kRows], found;
     __shared__ A piece_a[kSlices][kCols], piece_b[kSlices][kCols], state[kCols];
@@ -443,9 +443,12 @@ __global__ __launch_bounds__(TH) __attribute__((amdgpu_waves_per_eu(4))) void re
             const bool ends_group = tiles_before == kGroup - 1;
             if (threadIdx.x < kCols && real) Pair<A>::write(a.pieces + (tile * a.D + ch) * 2, ta, tb);
             A pa = 1, pb = 0, ja, jb;                        // the tiles before it in its group
-            join_share<kHelp>(a.pieces + (int64_t(group) * kGroup * a.D + ch) * 2, tiles_before, a.D, helper, ja, jb);
-            share_a[0][helper][column] = ja;
-            share_b[0][helper][column] = jb;
+            const bool helps = helper < kHelp;
+            if (helps) {
+                join_share<kHelp>(a.pieces + (int64_t(group) * kGroup * a.D + ch) * 2, tiles_before, a.D, helper, ja, jb);
+                share_a[0][helper][column] = ja;
+                share_b[0][helper][column] = jb;
+            }
             __syncthreads();
             for (int h = 0; h < kHelp; ++h) join(pa, pb, share_a[0][h][column], share_b[0][h][column]);
             if (ends_group && threadIdx.x < kCols && real) {
@@ -456,10 +459,12 @@ __global__ __launch_bounds__(TH) __attribute__((amdgpu_waves_per_eu(4))) void re
             A y = 0;
             if (group) {
                 const bool wait = !(pa < A(0));              // or a sequence begins in the group's part
-                join_share<kHelp>(a.groups + (int64_t(span) * kGroup * a.D + ch) * 2, wait ? groups_before : 0, a.D,
-                                  helper, ja, jb);
-                share_a[1][helper][column] = ja;
-                share_b[1][helper][column] = jb;
+                if (helps) {
+                    join_share<kHelp>(a.groups + (int64_t(span) * kGroup * a.D + ch) * 2, wait ? groups_before : 0,
+                                      a.D, helper, ja, jb);
+                    share_a[1][helper][column] = ja;
+                    share_b[1][helper][column] = jb;
+                }
                 __syncthreads();
                 if (threadIdx.x < kCols && real) {
                     A qa = 1, qb = 0;                        // the groups before it in its span
@@ -536,26 +541,30 @@ __global__ __launch_bounds__(TH) __attribute__((amdgpu_waves_per_eu(4))) void re
 // rows, of which half as many workgroups fit a CU) and where sequences are short: threads go to memory
 // for each sequence's first state one after the other (100,000 x 256 bf16, one row a sequence, 147 us
 // against 204, 25 rows 66 against 70; one sequence of 131,072 x 1,024 213 against 198).
-constexpr int kLanes = 16, kThreadsFew = 256, kThreadsMany = 512, kRowsFew = 4, kRowsMany = 8;
+constexpr int kThreadsFew = 256, kThreadsMany = 512, kRowsFew = 4, kRowsMany = 8;
 
-// How a call is cut: threads of a workgroup, rows of a thread, tiles along the rows, and whether they are
-// chained.
+// How a call is cut: threads of a workgroup, lanes across the channels, rows of a thread, tiles along the
+// rows, slabs across the channels, and whether the tiles are chained.
 struct Cut {
-    int threads, rows;
+    int threads, lanes, rows;
     bool chain;
-    int64_t tiles;
+    int64_t tiles, slabs;
 };
 
 // Large tiles from the size on where they give every CU a workgroup (20,000 x 512 bf16, 316 of
 // them, 30.5 us against 39 in small tiles; 5,000 x 256 fp32, 80 of them, 22 against 21).  No chain for
-// one or two small tiles.
+// one or two small tiles.  16 lanes across the channels (256 bytes of a row), or 8 where fewer of them
+// then lie past the row's end (50,001 x 301 bf16: 40 us against 47, 131,072 x 33: gradient 30
+// against 46); not for short sequences (100,000 x 256 in one-row ones 195 against 147).
 Cut cut(int64_t N, int64_t B, int64_t D, int V, bool grad) {
-    const int64_t slabs = (D + kLanes * V - 1) / (kLanes * V);
-    const int rows = grad || N < 32 * B ? kRowsFew : kRowsMany;
-    const int64_t few = kThreadsFew / kLanes * kRowsFew, many = kThreadsMany / kLanes * rows;
-    if (N <= 2 * few) return Cut{kThreadsFew, kRowsFew, false, (N + few - 1) / few};
-    if ((N + many - 1) / many * slabs < 256) return Cut{kThreadsFew, kRowsFew, true, (N + few - 1) / few};
-    return Cut{kThreadsMany, rows, true, (N + many - 1) / many};
+    const auto slabs = [&](int lanes) { return (D + lanes * V - 1) / (lanes * V); };
+    const bool brief = N < 32 * B;
+    const int rows = grad || brief ? kRowsFew : kRowsMany, lanes = !brief && slabs(8) < 2 * slabs(16) ? 8 : 16;
+    const int64_t few = kThreadsFew / 16 * kRowsFew, many = kThreadsMany / lanes * rows;
+    Cut k{kThreadsMany, lanes, rows, true, (N + many - 1) / many, slabs(lanes)};
+    if (N <= 2 * few || k.tiles * k.slabs < 256)
+        k = Cut{kThreadsFew, 16, kRowsFew, N > 2 * few, (N + few - 1) / few, slabs(16)};
+    return k;
 }
 
 // Channels of a thread: 16 bytes, or one where a row has less.
@@ -571,11 +580,10 @@ template <typename T, int V, bool GRAD>
 hipError_t launch(RecArgs<T> a, void *ws, hipStream_t st) {
     using A = typename Elem<T>::Acc;
     const Cut k = cut(a.N, a.B, a.D, V, GRAD);
-    const int64_t slabs = (a.D + kLanes * V - 1) / (kLanes * V);
     a.tiles = int(k.tiles);
     if (!k.chain) {
         gpps::TimedScope ts(st, GRAD ? "recurrence_grad" : "recurrence_fwd");
-        rec_kernel<T, V, GRAD, false, kThreadsFew, kLanes, kRowsFew><<<unsigned(slabs), kThreadsFew, 0, st>>>(a);
+        rec_kernel<T, V, GRAD, false, kThreadsFew, 16, kRowsFew><<<unsigned(k.slabs), kThreadsFew, 0, st>>>(a);
         return hipGetLastError();
     }
     const int64_t groups = groups_in(k.tiles), words = (2 * k.tiles + 2 * groups + groups_in(groups)) * a.D;
@@ -590,14 +598,16 @@ hipError_t launch(RecArgs<T> a, void *ws, hipStream_t st) {
     }
     gpps::TimedScope ts(st, GRAD ? "recurrence_grad" : "recurrence_fwd");
     // one workgroup a tile; the counter goes on over the launches of a call that needs several
-    for (int64_t left = k.tiles * slabs; left > 0; left -= kMostTiles) {
+    for (int64_t left = k.tiles * k.slabs; left > 0; left -= kMostTiles) {
         const unsigned blocks = unsigned(std::min(left, kMostTiles));
         if (k.threads == kThreadsFew)
-            rec_kernel<T, V, GRAD, true, kThreadsFew, kLanes, kRowsFew><<<blocks, kThreadsFew, 0, st>>>(a);
+            rec_kernel<T, V, GRAD, true, kThreadsFew, 16, kRowsFew><<<blocks, kThreadsFew, 0, st>>>(a);
+        else if (k.lanes == 8)
+            rec_kernel<T, V, GRAD, true, kThreadsMany, 8, GRAD ? kRowsFew : kRowsMany><<<blocks, kThreadsMany, 0, st>>>(a);
         else if (k.rows == kRowsFew)
-            rec_kernel<T, V, GRAD, true, kThreadsMany, kLanes, kRowsFew><<<blocks, kThreadsMany, 0, st>>>(a);
-        else if constexpr (!GRAD)
-            rec_kernel<T, V, false, true, kThreadsMany, kLanes, kRowsMany><<<blocks, kThreadsMany, 0, st>>>(a);
+            rec_kernel<T, V, GRAD, true, kThreadsMany, 16, kRowsFew><<<blocks, kThreadsMany, 0, st>>>(a);
+        else if constexpr (!GRAD && V > 1)                   // (rows of fewer than V channels fit 8 lanes)
+            rec_kernel<T, V, false, true, kThreadsMany, 16, kRowsMany><<<blocks, kThreadsMany, 0, st>>>(a);
         if (const hipError_t e = hipGetLastError()) return e;
     }
     return hipSuccess;

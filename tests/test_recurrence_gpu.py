@@ -306,3 +306,17 @@ def test_refusals():
     h, _ = gpps.recurrence(s["x"], s["gate"])
     with pytest.raises(ValueError):
         gpps.recurrence_grads(s["x"], s["gate"], h[:3], h)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f64"])
+@pytest.mark.parametrize("shape", ["long", "odd width", "short sequences"])
+def test_large_tiles(kind, shape):
+    """Enough rows for the large tiles: few long sequences over several groups and spans of them, a width that
+    leaves lanes past the row's end, and sequences of some twenty rows."""
+    if shape == "long":
+        check([0, 700, 41000], 256, kind, False, seed=20)
+    elif shape == "odd width":
+        check([0, 10, 27001], 270, kind, True, seed=21)
+    else:
+        cuts = sorted((i * 7919) % 27000 for i in range(1300))
+        check([0, 0] + cuts + [27000], 200, kind, False, seed=22)
