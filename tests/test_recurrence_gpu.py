@@ -320,3 +320,22 @@ def test_large_tiles(kind, shape):
     else:
         cuts = sorted((i * 7919) % 27000 for i in range(1300))
         check([0, 0] + cuts + [27000], 200, kind, False, seed=22)
+
+
+@pytest.mark.parametrize("reverse", [False, True])
+def test_memory_across_all_levels_of_the_chain(reverse):
+    """Memories of some 100,000 rows, so that the state reaches every tile through those before it."""
+    offsets, D = [0, 3, 280000], 6
+    s = make(offsets, D, "f64", seed=23)
+    s["gate"] = 11 + s["gate"] / 4
+    h, last = gpps.recurrence(s["x"], s["gate"], s["offsets"], s["h0"], reverse=reverse)
+    wh, wl, th, tl = ref.recurrence(f64(s["x"]), f64(s["gate"]), offsets, f64(s["h0"]), reverse, "f64")
+    assert float(np.abs(wl[1] - wh[100 if reverse else -100]).max()) < 0.5     # (slow, as meant)
+    close(h, wh, th, "h")
+    close(last, wl, tl, "h_last")
+    out = gpps.recurrence_grads(s["x"], s["gate"], h, s["dh"], s["offsets"], s["h0"], s["dh_last"], reverse=reverse)
+    dx, dg, d0, tx, tg, t0 = ref.recurrence_grads(f64(s["x"]), f64(s["gate"]), f64(h), f64(s["dh"]), offsets,
+                                                  f64(s["h0"]), f64(s["dh_last"]), reverse, "f64")
+    close(out["dx"], dx, tx, "dx")
+    close(out["dgate"], dg, tg, "dgate")
+    close(out["dh0"], d0, t0, "dh0")
