@@ -19,6 +19,7 @@ there.
 from __future__ import annotations
 
 import ctypes
+from array import array
 
 from . import F32, F64, GppsError, _check, _dev_tensor, lib, status_string
 
@@ -320,7 +321,8 @@ def _all_held(ts, what, dtype, sizes, device):
     """The addresses of a list's tensors, checked like _held (in passes over the list: a step of a small
     network is mostly its tensors' checks)."""
     k = len(ts)
-    if ([t.dtype for t in ts].count(dtype) != k or [t.device for t in ts].count(device) != k
+    on = device.index
+    if ([t.dtype for t in ts].count(dtype) != k or [t.get_device() for t in ts].count(on) != k
             or [t.numel() for t in ts] != sizes or not all([t.is_contiguous() for t in ts])):
         for i, (t, n) in enumerate(zip(ts, sizes)):
             _held(t, what, i, dtype, n, device)
@@ -392,9 +394,10 @@ def adamw_step(params, grads, m, v, step, lr, *, betas=(0.9, 0.999), eps=1e-8, w
     L = _lib()
     for dtype, gtype, sizes, held in calls:
         k = len(sizes)
-        arrays = [(ctypes.c_int64 * k)(*sizes)] + [(ctypes.c_void_p * k)(*a) for a in held] + [None] * (6 - len(held))
+        arrays = [array("q", sizes)] + [array("Q", a) for a in held]
+        at = [a.buffer_info()[0] for a in arrays] + [None] * (6 - len(held))
         bits = 8 if eight else 64 if dtype == torch.float64 else 32
-        _check(L.gpps_adamw(_row_dt(dtype), _row_dt(gtype), bits, k, *arrays, int(step), float(lr), float(betas[0]),
+        _check(L.gpps_adamw(_row_dt(dtype), _row_dt(gtype), bits, k, *at, int(step), float(lr), float(betas[0]),
                             float(betas[1]), float(eps), float(weight_decay), MAXIMIZE if maximize else 0, st))
 
 
