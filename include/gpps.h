@@ -272,7 +272,7 @@ gpps_status gpps_bound(gpps_dtype dt, int64_t N, int64_t M, int64_t Q, int64_t D
  *   - Arrays of rows have a stride: row n of `x` begins at x + n * ldx elements, ldx >= D.  A
  *     row's elements are neighbours.  Pointers need the element's alignment only.
  *   - N may be 0.  Outputs must not overlap inputs (the norm's y may be x).
- *   - 1 <= D <= GPPS_MAX_WIDTH, N D <= 2^40.
+ *   - 1 <= D <= GPPS_MAX_WIDTH, N D <= 2^40 (the recurrence: N <= 2^36 and B < 2^31 too).
  * Ownership, streams, errors and determinism are as above.
  */
 #define GPPS_MAX_WIDTH 16384

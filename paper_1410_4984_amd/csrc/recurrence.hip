@@ -623,7 +623,9 @@ bool aligned(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % 
 bool valid_dtype(gpps_dtype dt) { return dt == GPPS_F32 || dt == GPPS_F64 || dt == GPPS_BF16; }
 
 bool valid_shape(int64_t N, int64_t B, int64_t D) {
-    return N >= 0 && B >= 1 && B <= INT32_MAX && D >= 1 && D <= GPPS_MAX_WIDTH && N <= (int64_t(1) << 40) / D;
+    // (tiles and the chain's counter have 32 bits)
+    return N >= 0 && N <= int64_t(1) << 36 && B >= 1 && B <= INT32_MAX && D >= 1 && D <= GPPS_MAX_WIDTH &&
+           N <= (int64_t(1) << 40) / D;
 }
 
 size_t elem_size(gpps_dtype dt) { return dt == GPPS_F64 ? 8 : dt == GPPS_BF16 ? 2 : 4; }
