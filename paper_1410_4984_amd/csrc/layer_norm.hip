@@ -302,6 +302,7 @@ __global__ __launch_bounds__(1024) void ln_reduce_kernel(int64_t D, int parts, c
     const int64_t c = int64_t(blockIdx.x) * 16 + col;
     A s = 0;
     if (c < 2 * D)
+#pragma unroll 4
         for (int i = slice; i < parts; i += 64) s += part[int64_t(i) * 2 * D + c];
     sums[slice][col] = s;
     __syncthreads();

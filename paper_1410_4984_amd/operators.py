@@ -20,6 +20,7 @@ from __future__ import annotations
 
 import ctypes
 from array import array
+from operator import attrgetter
 
 from . import F32, F64, GppsError, _check, _dev_tensor, lib, status_string
 
@@ -317,16 +318,20 @@ def _held(t, what, i, dtype, n, device):
     return t.data_ptr()
 
 
+_dtype_of = attrgetter("dtype")
+
+
 def _all_held(ts, what, dtype, sizes, device):
-    """The addresses of a list's tensors, checked like _held (in passes over the list: a step of a small
-    network is mostly its tensors' checks)."""
+    """The addresses of a list's tensors, checked like _held (in passes over the list: a step over many
+    tensors is mostly their checks until its first launch)."""
+    import torch
+    T = torch.Tensor
     k = len(ts)
-    on = device.index
-    if ([t.dtype for t in ts].count(dtype) != k or [t.get_device() for t in ts].count(on) != k
-            or [t.numel() for t in ts] != sizes or not all([t.is_contiguous() for t in ts])):
+    if (list(map(_dtype_of, ts)).count(dtype) != k or list(map(T.get_device, ts)).count(device.index) != k
+            or list(map(T.numel, ts)) != sizes or not all(map(T.is_contiguous, ts))):
         for i, (t, n) in enumerate(zip(ts, sizes)):
             _held(t, what, i, dtype, n, device)
-    return [t.data_ptr() for t in ts]
+    return list(map(T.data_ptr, ts))
 
 
 def adamw_step(params, grads, m, v, step, lr, *, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01,
@@ -365,7 +370,7 @@ def adamw_step(params, grads, m, v, step, lr, *, betas=(0.9, 0.999), eps=1e-8, w
         raise ValueError(f"params must be GPU tensors (got {device})")
     if device.index != torch.cuda.current_device():
         raise ValueError(f"params are on {device}, which is not the current device")
-    types = [(p.dtype, g.dtype) for p, g in zip(params, lists[0])]
+    types = list(zip(map(_dtype_of, params), map(_dtype_of, lists[0])))
     calls, seen = [], []
     for dtype, gtype in dict.fromkeys(types):
         _row_dt(dtype)
