@@ -67,10 +67,12 @@ typedef enum { GPPS_F32 = 0, GPPS_F64 = 1, GPPS_BF16 = 2 } gpps_dtype;
 typedef enum {
     GPPS_OK = 0,
     GPPS_ERR_NULL = 1,      /* a required pointer is NULL                              */
-    GPPS_ERR_SHAPE = 2,     /* N < 1, M < 1, Q < 1, Q > GPPS_MAX_Q or M > GPPS_MAX_M   */
-    GPPS_ERR_HYPER = 3,     /* sigma_f2 or some l_q is not finite and > 0              */
+    GPPS_ERR_SHAPE = 2,     /* N < 1, M < 1, Q < 1, Q > GPPS_MAX_Q or M > GPPS_MAX_M; in
+                               the recognition operators a size, stride or count out of range */
+    GPPS_ERR_HYPER = 3,     /* sigma_f2 or some l_q is not finite and > 0; eps, or a constant
+                               of the AdamW step, out of range                         */
     GPPS_ERR_DTYPE = 4,     /* dt is not a gpps_dtype that the call takes              */
-    GPPS_ERR_WORKSPACE = 5, /* workspace smaller than gpps_workspace_bytes()           */
+    GPPS_ERR_WORKSPACE = 5, /* workspace smaller than the call's query returns         */
     GPPS_ERR_ALIGN = 6,     /* workspace not 256-byte aligned or an array misaligned   */
     GPPS_ERR_HIP = 7,       /* a HIP runtime call or kernel launch failed              */
     GPPS_ERR_PATH = 8       /* unknown flag bits, both path flags, or the requested path

@@ -12,6 +12,10 @@ fallback of any kind: if the library is missing or cannot run, calls raise.
     bound(mu, S, Z, Y, sigma_f2, l, beta, jitter)
                                        -> dict(L, dmu, dS, dZ, dsigma_f2, dl, dbeta)
 
+    layer_norm, recurrence (and their *_grads), adamw_step, AdamW, adamw_values
+                                       the operators of a recognition model (``operators``;
+                                       the model itself: ``recognition``)
+
 Notation follows the paper (section 2, Alg. 1-2): mu, S (variances) are N x Q,
 Z is M x Q, sigma_f2 the kernel variance, l the Q ARD lengthscales.  S = None
 means known inputs (every variance zero: the sparse GP regression case of
