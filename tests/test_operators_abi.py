@@ -65,6 +65,7 @@ def test_recurrence():
     for fn in (rec, rec_grads):
         assert fn(B=0) == SHAPE and fn(B=1 << 31) == SHAPE
         assert fn(off=None) == SHAPE                         # two sequences need offsets
+        assert fn(N=(1 << 36) + 1, D=1) == SHAPE             # past the tiles' counter
         assert fn(off=FAKE + 4) == ALIGN
         assert fn(g=None) == NULL and fn(h=None) == NULL and fn(ws=None) == NULL
         assert fn(ldg=7) == SHAPE and fn(ldh=7) == SHAPE
