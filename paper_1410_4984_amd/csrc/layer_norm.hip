@@ -407,10 +407,12 @@ int64_t groups_of(const Plan &p) { return p.tpr < 256 ? 256 / p.tpr : 1; }
 // Workgroups: a few on every CU, so that the memory has rows in flight while the weights are
 // loaded (and, in the gradient, partial rows written) few times.  50,000 x 1,024 bf16 forward 37.6 us
 // with up to 1,024, 50 with 512, 57 with 2,048; gradient 131,072 x 2,048 bf16 284 us with 768, 303 with
-// 512, 333 with 1,024.
+// 512, 333 with 1,024.  Past 768 groups of 2,048 rows there are more, so that a thread's sums of dw and db stay
+// that short (a sum of n terms one by one is off by up to n roundings).
 int64_t grad_blocks(int64_t N, const Plan &p) {
     const int64_t rows = groups_of(p);
-    return std::max<int64_t>(1, std::min<int64_t>((N + 4 * rows - 1) / (4 * rows), 768));
+    const int64_t most = std::min<int64_t>(std::max<int64_t>(N / (2048 * rows), 768), 65536);
+    return std::max<int64_t>(1, std::min<int64_t>((N + 4 * rows - 1) / (4 * rows), most));
 }
 
 template <typename T>
@@ -532,10 +534,12 @@ gpps_status gpps_layer_norm_grads(gpps_dtype dt, int64_t N, int64_t D, const voi
     hipStream_t st = static_cast<hipStream_t>(stream);
     const int acc = flags & GPPS_ACCUMULATE;
     const hipError_t e =
-        dt == GPPS_F32 ? run_gradient<float>(N, D, x, ldx, weight, mean, rstd, dy, lddy, dx, lddx, dweight, dbias, acc, workspace, st)
-        : dt == GPPS_F64
-            ? run_gradient<double>(N, D, x, ldx, weight, mean, rstd, dy, lddy, dx, lddx, dweight, dbias, acc, workspace, st)
-            : run_gradient<bf16_t>(N, D, x, ldx, weight, mean, rstd, dy, lddy, dx, lddx, dweight, dbias, acc, workspace, st);
+        dt == GPPS_F32 ? run_gradient<float>(N, D, x, ldx, weight, mean, rstd, dy, lddy, dx, lddx, dweight, dbias, acc,
+                                             workspace, st)
+        : dt == GPPS_F64 ? run_gradient<double>(N, D, x, ldx, weight, mean, rstd, dy, lddy, dx, lddx, dweight, dbias,
+                                                acc, workspace, st)
+                         : run_gradient<bf16_t>(N, D, x, ldx, weight, mean, rstd, dy, lddy, dx, lddx, dweight, dbias,
+                                                acc, workspace, st);
     return e == hipSuccess ? GPPS_OK : GPPS_ERR_HIP;
 }
 

@@ -215,3 +215,23 @@ def test_refusals():
         gpps.layer_norm_grads(x, w, mean[:3], rstd, dy)
     with pytest.raises(ValueError):
         gpps.layer_norm_grads(x, w, mean, rstd, dy, workspace=torch.empty(8, dtype=torch.uint8, device=DEV))
+
+
+def test_sums_over_millions_of_rows():
+    """float32 sums over so many rows that there are more workgroups than usual."""
+    N, D = 7_000_003, 300
+    x = torch.randn(N, D, device=DEV)
+    y, mean, rstd = gpps.layer_norm(x)
+    dy = y.fill_(0.1)
+    out = gpps.layer_norm_grads(x, torch.ones(D, device=DEV), mean, rstd, dy)
+    tenth = float(torch.tensor(0.1))
+    exact, size = torch.zeros(D, dtype=torch.float64, device=DEV), torch.zeros(D, dtype=torch.float64, device=DEV)
+    for part in torch.arange(N, device=DEV).split(1_000_000):
+        t = tenth * (x[part].double() - mean[part, None].double()) * rstd[part, None].double()
+        exact += t.sum(0)
+        size += t.abs().sum(0)
+    # a thread adds some 2,048 terms one by one at most, the rest in 64 slices and trees: fewer than 3,000 roundings
+    # on the longest way
+    tol = 3000 * 2.0 ** -24
+    assert float((out["dbias"].double() - N * tenth).abs().max()) < tol * N * tenth
+    assert bool(((out["dweight"].double() - exact).abs() < tol * size).all())
