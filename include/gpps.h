@@ -315,6 +315,7 @@ gpps_status gpps_layer_norm_grads(gpps_dtype dt, int64_t N, int64_t D, const voi
  *                     never fall and end with N.  The call cannot check that: other contents
  *                     give unspecified results, but no access outside the arrays.
  * States are independent between sequences: what is not finite in one stays in it.
+ * A call whose workspace query returns 256 does not write to its workspace.
  */
 size_t gpps_recurrence_workspace_bytes(gpps_dtype dt, int64_t N, int64_t B, int64_t D);
 gpps_status gpps_recurrence(gpps_dtype dt, int64_t N, int64_t B, int64_t D, const void *x,

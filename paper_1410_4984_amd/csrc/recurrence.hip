@@ -582,7 +582,7 @@ int vector_of(gpps_dtype dt, int64_t D) {
     return D < V ? 1 : V;
 }
 
-constexpr size_t kCounterBytes = 256;
+constexpr size_t kCounterBytes = 256;           // calls without a chain ask for no more, and don't touch it
 constexpr int64_t kMostTiles = 1 << 22;          // of one launch (its threads are counted in 32 bits)
 
 template <typename T, int V, bool GRAD>

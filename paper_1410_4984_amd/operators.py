@@ -19,24 +19,31 @@ there.
 from __future__ import annotations
 
 import ctypes
+import functools
 from array import array
 from operator import attrgetter
 
-from . import F32, F64, GppsError, _check, _dev_tensor, lib, status_string
+from . import F32, F64, GppsError, _check, lib, status_string
 
 BF16 = 2
 ACCUMULATE, REVERSE, MAXIMIZE = 1, 8, 16
 MAX_WIDTH = 16384
 ADAMW_BLOCK = 256
 
-_declared = None
+# The smallest calls are mostly host time, so what every call needs is looked up once: torch (imported
+# with the first call, as in the rest of the package), the library, and for each row type its code
+# and the type of sums, states and parameters beside it.
+torch = None
+_L = None
+_TYPES = {}
 
 
 def _lib():
     """The library with the argument types of these entry points set."""
-    global _declared
-    if _declared is not None:
-        return _declared
+    global torch, _L
+    if _L is not None:
+        return _L
+    import torch as t
     L = lib()
     i64, vp, d, sz, i32 = ctypes.c_int64, ctypes.c_void_p, ctypes.c_double, ctypes.c_size_t, ctypes.c_int
     L.gpps_layer_norm.argtypes = [i32, i64, i64, vp, i64, vp, vp, d, vp, i64, vp, vp, vp]
@@ -53,55 +60,63 @@ def _lib():
     L.gpps_adamw_values.argtypes = [i32, i64, vp, vp, vp, vp]
     for name in ("layer_norm", "layer_norm_grads", "recurrence", "recurrence_grads", "adamw", "adamw_values"):
         getattr(L, "gpps_" + name).restype = i32
-    _declared = L
+    _TYPES.update({t.float32: (F32, t.float32), t.float64: (F64, t.float64), t.bfloat16: (BF16, t.float32)})
+    torch, _L = t, L
     return L
 
 
-def _row_dt(dtype) -> int:
-    import torch
-    if dtype == torch.float32:
-        return F32
-    if dtype == torch.float64:
-        return F64
-    if dtype == torch.bfloat16:
-        return BF16
-    raise TypeError(f"unsupported dtype {dtype}")
-
-
-def _wide(dtype):
-    import torch
-    return torch.float64 if dtype == torch.float64 else torch.float32
+def _types(dtype):
+    """The code of a row type and the type of sums, states and parameters beside it."""
+    try:
+        return _TYPES[dtype]
+    except KeyError:
+        raise TypeError(f"unsupported dtype {dtype}") from None
 
 
 def _first(x, name):
-    """Type, device and shape of the array that the others are checked against."""
-    import torch
+    """The array that the others are checked against: its types, device, shape and row stride."""
     if not isinstance(x, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
-    if x.device.type != "cuda":
-        raise ValueError(f"{name} must be a GPU tensor (got {x.device})")
-    if x.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {x.device}, which is not the current device")
-    if x.dim() != 2:
-        raise ValueError(f"{name}: expected rows [N, D], got shape {tuple(x.shape)}")
-    return x.dtype, x.device, x.shape[0], x.shape[1]
+    device = x.device
+    if device.type != "cuda":
+        raise ValueError(f"{name} must be a GPU tensor (got {device})")
+    if device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {device}, which is not the current device")
+    shape = x.shape
+    if len(shape) != 2:
+        raise ValueError(f"{name}: expected rows [N, D], got shape {tuple(shape)}")
+    dtype = x.dtype
+    dt, wide = _types(dtype)
+    return dt, dtype, wide, device, shape, _ld(x, name, dtype, shape, device)
 
 
 def _ld(x, name, dtype, shape, device) -> int:
     """Checks an array of rows and returns the stride of its rows."""
-    import torch
     if not isinstance(x, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if x.dtype != dtype or x.device != device:
         raise ValueError(f"{name}: expected {dtype} on {device}, got {x.dtype} on {x.device}")
     if x.shape != shape:
-        raise ValueError(f"{name}: expected shape {shape}, got {tuple(x.shape)}")
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(x.shape)}")
     N, D = shape
     row, one = x.stride()
     if (D > 1 and one != 1) or (N > 1 and row < D):
         raise ValueError(f"{name}: a row's elements must be neighbours and rows must not overlap "
                          f"(strides {x.stride()})")
     return row if N > 1 else D
+
+
+def _dense(x, name, dtype, shape, device) -> int:
+    """Checks a contiguous array and returns its address."""
+    if not isinstance(x, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if x.dtype != dtype or x.device != device:
+        raise ValueError(f"{name}: expected {dtype} on {device}, got {x.dtype} on {x.device}")
+    if x.shape != shape:
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(x.shape)}")
+    if not x.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return x.data_ptr()
 
 
 def _ptr(x):
@@ -111,13 +126,11 @@ def _ptr(x):
 def _current(device) -> int:
     """The current stream's handle (what torch.cuda.current_stream(device).cuda_stream is, without
     its 2 us)."""
-    import torch
     return torch._C._cuda_getCurrentRawStream(device.index)
 
 
 def _on_stream(stream, tensors, call):
     """call() with `stream` as the current one; the tensors' memory is kept until it is done with them."""
-    import torch
     for t in tensors:
         if isinstance(t, torch.Tensor) and t.device.type == "cuda":
             t.record_stream(stream)
@@ -126,7 +139,6 @@ def _on_stream(stream, tensors, call):
 
 
 def _scratch(need, workspace, device):
-    import torch
     if need == 0:
         raise GppsError(2, status_string(2))
     if workspace is None:
@@ -141,39 +153,45 @@ def _scratch(need, workspace, device):
 
 # ------------------------------------------------------------------ layer norm
 
+@functools.lru_cache(maxsize=256)
+def _norm_bytes(dt: int, N: int, D: int) -> int:
+    return int(_L.gpps_layer_norm_workspace_bytes(dt, N, D))
+
+
 def layer_norm(x, weight=None, bias=None, eps=1e-5, *, out=None, stream=None):
     """Layer norm of the rows of x [N x D].
 
     Returns (y [N x D], mean [N], rstd [N]); ``out`` is such a triple to write into
     (y may be x)."""
-    import torch
+    L = _L or _lib()
     if stream is not None:
         return _on_stream(stream, (x, weight, bias, *(out or ())),
                           lambda: layer_norm(x, weight, bias, eps, out=out))
-    dtype, device, N, D = _first(x, "x")
-    dt, wide = _row_dt(dtype), _wide(dtype)
-    ldx = _ld(x, "x", dtype, (N, D), device)
+    dt, dtype, wide, device, shape, ldx = _first(x, "x")
+    N, D = shape
+    w = b = None
     if weight is not None:
-        _dev_tensor(weight, "weight", wide, (D,), device)
+        w = _dense(weight, "weight", wide, (D,), device)
     if bias is not None:
-        _dev_tensor(bias, "bias", wide, (D,), device)
+        b = _dense(bias, "bias", wide, (D,), device)
     if out is None:
-        y = torch.empty((N, D), dtype=dtype, device=device)
-        mean = torch.empty(N, dtype=wide, device=device)
-        rstd = torch.empty(N, dtype=wide, device=device)
-        ldy = D
+        y, ldy = x.new_empty(shape), D
+        mean, rstd = x.new_empty(N, dtype=wide), x.new_empty(N, dtype=wide)
+        m, r = mean.data_ptr(), rstd.data_ptr()
     else:
         y, mean, rstd = out
-        ldy = _ld(y, "y", dtype, (N, D), device)
-        _dev_tensor(mean, "mean", wide, (N,), device)
-        _dev_tensor(rstd, "rstd", wide, (N,), device)
-    _check(_lib().gpps_layer_norm(dt, N, D, x.data_ptr(), ldx, _ptr(weight), _ptr(bias), float(eps), y.data_ptr(),
-                                  ldy, mean.data_ptr(), rstd.data_ptr(), _current(device)))
+        ldy = _ld(y, "y", dtype, shape, device)
+        m = _dense(mean, "mean", wide, (N,), device)
+        r = _dense(rstd, "rstd", wide, (N,), device)
+    status = L.gpps_layer_norm(dt, N, D, x.data_ptr(), ldx, w, b, eps, y.data_ptr(), ldy, m, r, _current(device))
+    if status:
+        _check(status)
     return y, mean, rstd
 
 
 def layer_norm_workspace_bytes(dtype, N: int, D: int) -> int:
-    return int(_lib().gpps_layer_norm_workspace_bytes(_row_dt(dtype), N, D))
+    _lib()
+    return _norm_bytes(_types(dtype)[0], N, D)
 
 
 def layer_norm_grads(x, weight, mean, rstd, dy, *, bias=True, accumulate=False, out=None, workspace=None,
@@ -183,55 +201,76 @@ def layer_norm_grads(x, weight, mean, rstd, dy, *, bias=True, accumulate=False, 
     Returns a dict with dx [N x D], dweight [D] (None when weight is None) and dbias
     [D] (None with ``bias=False``).  With ``accumulate=True`` and ``out`` (such a
     dict) dweight and dbias are added to."""
-    import torch
+    L = _L or _lib()
     if stream is not None:
         return _on_stream(stream, (x, weight, mean, rstd, dy, workspace, *(out or {}).values()),
                           lambda: layer_norm_grads(x, weight, mean, rstd, dy, bias=bias, accumulate=accumulate,
                                                    out=out, workspace=workspace))
-    dtype, device, N, D = _first(x, "x")
-    dt, wide = _row_dt(dtype), _wide(dtype)
-    ldx = _ld(x, "x", dtype, (N, D), device)
-    lddy = _ld(dy, "dy", dtype, (N, D), device)
+    dt, dtype, wide, device, shape, ldx = _first(x, "x")
+    N, D = shape
+    lddy = _ld(dy, "dy", dtype, shape, device)
+    w = None
     if weight is not None:
-        _dev_tensor(weight, "weight", wide, (D,), device)
-    _dev_tensor(mean, "mean", wide, (N,), device)
-    _dev_tensor(rstd, "rstd", wide, (N,), device)
+        w = _dense(weight, "weight", wide, (D,), device)
+    m = _dense(mean, "mean", wide, (N,), device)
+    r = _dense(rstd, "rstd", wide, (N,), device)
     if out is None:
-        new = torch.zeros if accumulate else torch.empty
-        out = {"dx": torch.empty((N, D), dtype=dtype, device=device),
-               "dweight": new(D, dtype=wide, device=device) if weight is not None else None,
-               "dbias": new(D, dtype=wide, device=device) if bias else None}
+        new = x.new_zeros if accumulate else x.new_empty
+        out = {"dx": x.new_empty(shape), "dweight": new(D, dtype=wide) if weight is not None else None,
+               "dbias": new(D, dtype=wide) if bias else None}
+        lddx = D
     else:
         for k in ("dweight", "dbias"):
             if out[k] is not None:
-                _dev_tensor(out[k], k, wide, (D,), device)
-    lddx = _ld(out["dx"], "dx", dtype, (N, D), device)
-    ws, ws_bytes = _scratch(layer_norm_workspace_bytes(dtype, N, D), workspace, device)
-    _check(_lib().gpps_layer_norm_grads(
-        dt, N, D, x.data_ptr(), ldx, _ptr(weight), mean.data_ptr(), rstd.data_ptr(), dy.data_ptr(), lddy,
-        out["dx"].data_ptr(), lddx, _ptr(out["dweight"]), _ptr(out["dbias"]), ACCUMULATE if accumulate else 0,
-        ws.data_ptr(), ws_bytes, _current(device)))
+                _dense(out[k], k, wide, (D,), device)
+        lddx = _ld(out["dx"], "dx", dtype, shape, device)
+    ws, ws_bytes = _scratch(_norm_bytes(dt, N, D), workspace, device)
+    status = L.gpps_layer_norm_grads(
+        dt, N, D, x.data_ptr(), ldx, w, m, r, dy.data_ptr(), lddy, out["dx"].data_ptr(), lddx, _ptr(out["dweight"]),
+        _ptr(out["dbias"]), ACCUMULATE if accumulate else 0, ws.data_ptr(), ws_bytes, _current(device))
+    if status:
+        _check(status)
     return out
 
 
 # ------------------------------------------------------------------ recurrence
 
+@functools.lru_cache(maxsize=256)
+def _recurrence_bytes(dt: int, N: int, B: int, D: int) -> int:
+    return int(_L.gpps_recurrence_workspace_bytes(dt, N, B, D))
+
+
+# A recurrence without a chain (of few rows) asks for the least workspace, 256 bytes, and leaves it alone:
+# one for each device does for all such calls.
+_CHAINLESS = 256
+_untouched = {}
+
+
+def _recurrence_scratch(need, workspace, device):
+    if workspace is not None or need != _CHAINLESS:
+        return _scratch(need, workspace, device)
+    if device not in _untouched:
+        _untouched[device] = torch.empty(_CHAINLESS, dtype=torch.uint8, device=device)
+    return _untouched[device], need
+
+
 def recurrence_workspace_bytes(dtype, N: int, B: int, D: int) -> int:
-    return int(_lib().gpps_recurrence_workspace_bytes(_row_dt(dtype), N, B, D))
+    _lib()
+    return _recurrence_bytes(_types(dtype)[0], N, B, D)
 
 
-def _sequences(offsets, device) -> int:
-    """Checks the offsets (their contents are the caller's, on the device) and returns how many sequences they mark."""
-    import torch
+def _sequences(offsets, device):
+    """Checks the offsets (their contents are the caller's, on the device) and returns how many sequences they mark
+    and their address."""
     if offsets is None:
-        return 1
+        return 1, None
     if not isinstance(offsets, torch.Tensor):
         raise TypeError("offsets must be a torch.Tensor")
     if offsets.device != device or offsets.dtype != torch.int64:
         raise ValueError(f"offsets: expected torch.int64 on {device}, got {offsets.dtype} on {offsets.device}")
     if offsets.dim() != 1 or offsets.shape[0] < 2 or not offsets.is_contiguous():
         raise ValueError("offsets: expected contiguous [B + 1] with B >= 1")
-    return offsets.shape[0] - 1
+    return offsets.shape[0] - 1, offsets.data_ptr()
 
 
 def recurrence(x, gate, offsets=None, h0=None, *, reverse=False, out=None, workspace=None, stream=None):
@@ -243,29 +282,28 @@ def recurrence(x, gate, offsets=None, h0=None, *, reverse=False, out=None, works
     rows (None: zero).  Returns (h [N x D], h_last [B x D]), h_last the states after
     the last rows, so a stream of rows is taken in pieces (down to one row a call) by
     handing h_last on as h0.  ``reverse=True`` takes rows from last to first."""
-    import torch
+    L = _L or _lib()
     if stream is not None:
         return _on_stream(stream, (x, gate, offsets, h0, workspace, *(out or ())),
                           lambda: recurrence(x, gate, offsets, h0, reverse=reverse, out=out, workspace=workspace))
-    dtype, device, N, D = _first(x, "x")
-    dt, wide = _row_dt(dtype), _wide(dtype)
-    ldx = _ld(x, "x", dtype, (N, D), device)
-    ldg = _ld(gate, "gate", dtype, (N, D), device)
-    B = _sequences(offsets, device)
-    if h0 is not None:
-        _dev_tensor(h0, "h0", wide, (B, D), device)
+    dt, dtype, wide, device, shape, ldx = _first(x, "x")
+    N, D = shape
+    ldg = _ld(gate, "gate", dtype, shape, device)
+    B, off = _sequences(offsets, device)
+    h0p = None if h0 is None else _dense(h0, "h0", wide, (B, D), device)
     if out is None:
-        h = torch.empty((N, D), dtype=dtype, device=device)
-        h_last = torch.empty((B, D), dtype=wide, device=device)
-        ldh = D
+        h, ldh = x.new_empty(shape), D
+        h_last = x.new_empty((B, D), dtype=wide)
+        last = h_last.data_ptr()
     else:
         h, h_last = out
-        ldh = _ld(h, "h", dtype, (N, D), device)
-        _dev_tensor(h_last, "h_last", wide, (B, D), device)
-    ws, ws_bytes = _scratch(recurrence_workspace_bytes(dtype, N, B, D), workspace, device)
-    _check(_lib().gpps_recurrence(dt, N, B, D, x.data_ptr(), ldx, gate.data_ptr(), ldg, _ptr(offsets), _ptr(h0),
-                                  h.data_ptr(), ldh, h_last.data_ptr(), REVERSE if reverse else 0, ws.data_ptr(),
-                                  ws_bytes, _current(device)))
+        ldh = _ld(h, "h", dtype, shape, device)
+        last = _dense(h_last, "h_last", wide, (B, D), device)
+    ws, ws_bytes = _recurrence_scratch(_recurrence_bytes(dt, N, B, D), workspace, device)
+    status = L.gpps_recurrence(dt, N, B, D, x.data_ptr(), ldx, gate.data_ptr(), ldg, off, h0p, h.data_ptr(), ldh,
+                               last, REVERSE if reverse else 0, ws.data_ptr(), ws_bytes, _current(device))
+    if status:
+        _check(status)
     return h, h_last
 
 
@@ -276,36 +314,34 @@ def recurrence_grads(x, gate, h, dh, offsets=None, h0=None, dh_last=None, *, rev
 
     Returns a dict with dx, dgate [N x D] and dh0 [B x D]; ``out`` is such a dict to
     write into (its dh0 may be None)."""
-    import torch
+    L = _L or _lib()
     if stream is not None:
         return _on_stream(stream, (x, gate, h, dh, offsets, h0, dh_last, workspace, *(out or {}).values()),
                           lambda: recurrence_grads(x, gate, h, dh, offsets, h0, dh_last, reverse=reverse, out=out,
                                                    workspace=workspace))
-    dtype, device, N, D = _first(x, "x")
-    dt, wide = _row_dt(dtype), _wide(dtype)
-    ldx = _ld(x, "x", dtype, (N, D), device)
-    ldg = _ld(gate, "gate", dtype, (N, D), device)
-    ldh = _ld(h, "h", dtype, (N, D), device)
-    lddh = D if dh is None else _ld(dh, "dh", dtype, (N, D), device)
-    B = _sequences(offsets, device)
-    for t, name in ((h0, "h0"), (dh_last, "dh_last")):
-        if t is not None:
-            _dev_tensor(t, name, wide, (B, D), device)
+    dt, dtype, wide, device, shape, ldx = _first(x, "x")
+    N, D = shape
+    ldg = _ld(gate, "gate", dtype, shape, device)
+    ldh = _ld(h, "h", dtype, shape, device)
+    lddh = D if dh is None else _ld(dh, "dh", dtype, shape, device)
+    B, off = _sequences(offsets, device)
+    h0p = None if h0 is None else _dense(h0, "h0", wide, (B, D), device)
+    dlp = None if dh_last is None else _dense(dh_last, "dh_last", wide, (B, D), device)
     if out is None:
-        out = {"dx": torch.empty((N, D), dtype=dtype, device=device),
-               "dgate": torch.empty((N, D), dtype=dtype, device=device),
-               "dh0": torch.empty((B, D), dtype=wide, device=device)}
+        out = {"dx": x.new_empty(shape), "dgate": x.new_empty(shape), "dh0": x.new_empty((B, D), dtype=wide)}
         lddx = lddg = D
     else:
-        lddx = _ld(out["dx"], "dx", dtype, (N, D), device)
-        lddg = _ld(out["dgate"], "dgate", dtype, (N, D), device)
+        lddx = _ld(out["dx"], "dx", dtype, shape, device)
+        lddg = _ld(out["dgate"], "dgate", dtype, shape, device)
         if out["dh0"] is not None:
-            _dev_tensor(out["dh0"], "dh0", wide, (B, D), device)
-    ws, ws_bytes = _scratch(recurrence_workspace_bytes(dtype, N, B, D), workspace, device)
-    _check(_lib().gpps_recurrence_grads(
-        dt, N, B, D, x.data_ptr(), ldx, gate.data_ptr(), ldg, h.data_ptr(), ldh, _ptr(dh), lddh, _ptr(offsets),
-        _ptr(h0), _ptr(dh_last), out["dx"].data_ptr(), lddx, out["dgate"].data_ptr(), lddg, _ptr(out["dh0"]),
-        REVERSE if reverse else 0, ws.data_ptr(), ws_bytes, _current(device)))
+            _dense(out["dh0"], "dh0", wide, (B, D), device)
+    ws, ws_bytes = _recurrence_scratch(_recurrence_bytes(dt, N, B, D), workspace, device)
+    status = L.gpps_recurrence_grads(
+        dt, N, B, D, x.data_ptr(), ldx, gate.data_ptr(), ldg, h.data_ptr(), ldh, _ptr(dh), lddh, off, h0p, dlp,
+        out["dx"].data_ptr(), lddx, out["dgate"].data_ptr(), lddg, _ptr(out["dh0"]), REVERSE if reverse else 0,
+        ws.data_ptr(), ws_bytes, _current(device))
+    if status:
+        _check(status)
     return out
 
 
@@ -324,7 +360,6 @@ _dtype_of = attrgetter("dtype")
 def _all_held(ts, what, dtype, sizes, device):
     """The addresses of a list's tensors, checked like _held (in passes over the list: a step over many
     tensors is mostly their checks until its first launch)."""
-    import torch
     T = torch.Tensor
     k = len(ts)
     if (list(map(_dtype_of, ts)).count(dtype) != k or list(map(T.get_device, ts)).count(device.index) != k
@@ -347,7 +382,7 @@ def adamw_step(params, grads, m, v, step, lr, *, betas=(0.9, 0.999), eps=1e-8, w
     ``m_scale`` and ``v_scale``, 8-bit codes: m int8, v uint8, and a float32 scale for
     each block of 256 elements (``AdamW(bits=8)`` makes them; ``adamw_values`` reads
     them).  Every tensor is contiguous and none overlaps another."""
-    import torch
+    L = _L or _lib()
     if stream is not None:
         every = [t for l in (params, grads, m, v, m_scale or (), v_scale or ()) for t in l]
         return _on_stream(stream, every, lambda: adamw_step(
@@ -373,7 +408,7 @@ def adamw_step(params, grads, m, v, step, lr, *, betas=(0.9, 0.999), eps=1e-8, w
     types = list(zip(map(_dtype_of, params), map(_dtype_of, lists[0])))
     calls, seen = [], []
     for dtype, gtype in dict.fromkeys(types):
-        _row_dt(dtype)
+        dt, wide = _types(dtype)
         if gtype != dtype and {dtype, gtype} != {torch.float32, torch.bfloat16}:
             raise TypeError(f"gradients of {gtype} beside parameters of {dtype}")
         if eight and dtype == torch.float64:
@@ -383,7 +418,6 @@ def adamw_step(params, grads, m, v, step, lr, *, betas=(0.9, 0.999), eps=1e-8, w
             at = [i for i, t in enumerate(types) if t == (dtype, gtype)]
             mine = [[l[i] for i in at] for l in mine]
         sizes = [p.numel() for p in mine[0]]
-        wide = _wide(dtype)
         held = [_all_held(mine[0], "params", dtype, sizes, device), _all_held(mine[1], "grads", gtype, sizes, device),
                 _all_held(mine[2], "m", torch.int8 if eight else wide, sizes, device),
                 _all_held(mine[3], "v", torch.uint8 if eight else wide, sizes, device)]
@@ -392,24 +426,23 @@ def adamw_step(params, grads, m, v, step, lr, *, betas=(0.9, 0.999), eps=1e-8, w
             held += [_all_held(mine[4], "m_scale", torch.float32, blocks, device),
                      _all_held(mine[5], "v_scale", torch.float32, blocks, device)]
         seen += [q for q, n in zip(held[0], sizes) if n]
-        calls.append((dtype, gtype, sizes, held))
+        calls.append((dt, _types(gtype)[0], sizes, held))
     if len(set(seen)) < len(seen):
         raise ValueError("a tensor is listed twice")
     st = _current(device)
-    L = _lib()
-    for dtype, gtype, sizes, held in calls:
+    for dt, gdt, sizes, held in calls:
         k = len(sizes)
         arrays = [array("q", sizes)] + [array("Q", a) for a in held]
         at = [a.buffer_info()[0] for a in arrays] + [None] * (6 - len(held))
-        bits = 8 if eight else 64 if dtype == torch.float64 else 32
-        _check(L.gpps_adamw(_row_dt(dtype), _row_dt(gtype), bits, k, *at, int(step), float(lr), float(betas[0]),
+        bits = 8 if eight else 64 if dt == F64 else 32
+        _check(L.gpps_adamw(dt, gdt, bits, k, *at, int(step), float(lr), float(betas[0]),
                             float(betas[1]), float(eps), float(weight_decay), MAXIMIZE if maximize else 0, st))
 
 
 def adamw_values(codes, scale, *, out=None, stream=None):
     """The float32 values that 8-bit moments stand for: of a first moment (int8 codes) or
     a second one (uint8), with their scales."""
-    import torch
+    L = _L or _lib()
     if stream is not None:
         return _on_stream(stream, (codes, scale, out), lambda: adamw_values(codes, scale, out=out))
     if codes.dtype not in (torch.int8, torch.uint8):
@@ -422,8 +455,8 @@ def adamw_values(codes, scale, *, out=None, stream=None):
     if out is None:
         out = torch.empty(codes.shape, dtype=torch.float32, device=device)
     else:
-        _dev_tensor(out, "out", torch.float32, tuple(codes.shape), device)
-    _check(_lib().gpps_adamw_values(1 if codes.dtype == torch.uint8 else 0, n, codes.data_ptr(), scale.data_ptr(),
+        _dense(out, "out", torch.float32, codes.shape, device)
+    _check(L.gpps_adamw_values(1 if codes.dtype == torch.uint8 else 0, n, codes.data_ptr(), scale.data_ptr(),
                                     out.data_ptr(), _current(device)))
     return out
 
@@ -438,7 +471,7 @@ class AdamW:
 
     def __init__(self, params, lr=1e-3, *, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, bits=32,
                  maximize=False):
-        import torch
+        _lib()
         if bits not in (8, 32):
             raise ValueError(f"bits: 8 or 32, got {bits}")
         self.params = list(params)
@@ -451,7 +484,7 @@ class AdamW:
             self.m_scale, self.v_scale = ([torch.zeros(-(-p.numel() // ADAMW_BLOCK), dtype=torch.float32,
                                                        device=p.device) for p in self.params] for _ in range(2))
         else:
-            self.m, self.v = ([torch.zeros_like(p, dtype=_wide(p.dtype)) for p in self.params] for _ in range(2))
+            self.m, self.v = ([torch.zeros_like(p, dtype=_types(p.dtype)[1]) for p in self.params] for _ in range(2))
 
     def step(self, grads, *, lr=None, stream=None):
         """One step with one gradient a parameter (None: that parameter is left as it is)."""
